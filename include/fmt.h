@@ -35,6 +35,7 @@
  *   fmt_conv2d_*   convolution forward / dgrad / wgrad as the same product on patches gathered on the fly
  *   fmt_dls_step   loss-scale controller and denormal-fraction monitor on the device (Sec. II, Sec. V)
  *   fmt_quantize_static   fmt_quantize for callers that cannot allocate device memory
+ *   fmt_dropout / fmt_layernorm_* / fmt_attention_*   what a transformer layer computes beside its products
  *
  * Conventions common to all calls
  *   - Every data pointer is a DEVICE pointer owned by the caller.  The library never
@@ -512,6 +513,83 @@ typedef struct fmt_dls_params {
 int fmt_dls_init(fmt_dls_state_t *state, float loss_scale, void *stream);
 int fmt_dls_step(const fmt_hist_t *hists, int64_t count, fmt_dls_params_t prm,
                  fmt_dls_state_t *state, void *stream);
+
+/*
+ * What a transformer layer computes beside its products: dropout, dropout + residual + layer norm, attention.
+ * Sec. IV-A rounds the inputs and the outputs of every layer and nothing inside it; so do these.  R is the rounding of
+ * fmt_quantize, and everything between two R is held in fp32.
+ *
+ * store   how tensors are read: FMT_STORE_F32, fp32 that is rounded by R as it is read; FMT_STORE_CODE16, codes of
+ *         fmt_pack16 (1 + e + m <= 16), taken for the values that fmt_unpack16 gives.  Codes of 1/5/10 are IEEE
+ *         half, those of 1/8/7 bfloat16.  Weights and biases are fp32 either way, rounded as they are read.
+ * result  how tensors are written: FMT_RESULT_F32, unrounded fp32, as fmt_gemm gives; FMT_RESULT_ROUND, R of that in
+ *         fp32; FMT_RESULT_CODE16, its codes.  Statistics of rows and gradients of parameters are unrounded fp32.
+ *
+ * Leading dimensions and strides are in elements; tensors need the alignment of their elements and no more.
+ * Outputs must not overlap inputs or one another, unless stated otherwise.
+ */
+#define FMT_STORE_F32 0
+#define FMT_STORE_CODE16 1
+#define FMT_RESULT_F32 0
+#define FMT_RESULT_ROUND 1
+#define FMT_RESULT_CODE16 2
+
+/*
+ * Dropout whose mask is made from a counter wherever it is needed and never stored.  Element (row, col) of a tensor of
+ * `cols` columns takes 16 bits of Philox-4x32 (ten rounds; Salmon et al., 2011) with
+ *   counter  (n mod 2^32, n / 2^32, step mod 2^32, site),  n = row * ceil(cols / 8) + col / 8
+ *   key      (seed mod 2^32, seed / 2^32)
+ * namely half col % 2 (the low one first) of word (col % 8) / 2 of the result.  With L = p * 65536 rounded to the nearest
+ * integer, an element is kept, and multiplied by 65536 / (65536 - L) rounded to fp32, where its 16 bits are >= L, and
+ * replaced by +0 (whatever it was: infinities and NaN too) where they are less.
+ *   p     0 <= p <= 1, dropped share; 0 drops nothing
+ *   site  tells the dropouts of one step apart
+ *   rng   device, two uint64_t {seed, step}, 8-byte aligned; read by the kernel, so a program may change them on the
+ *         stream between steps, also between replays of a recorded graph.  May be NULL with p == 0 in the layer norm.
+ * The backward pass makes the same bits from the same (rng, site) and the same shape.
+ */
+typedef struct fmt_dropout {
+    float p;
+    uint32_t site;
+    const uint64_t *rng;
+} fmt_dropout_t;
+
+/*
+ * fmt_dropout -- y = D(R(x)), rows x cols; its backward pass is the same call on the gradient.  y may be x itself (same
+ * address, leading dimension and element size).  rows or cols equal to 0 succeeds.  p outside [0, 1]: FMT_ERR_RANGE.
+ */
+int fmt_dropout(const void *x, int64_t ldx, void *y, int64_t ldy, int64_t rows, int64_t cols, fmt_dropout_t d,
+                int32_t store, int32_t result, fmt_format_t f, void *stream);
+
+/*
+ * fmt_layernorm_fwd -- what stands between two sublayers:
+ *   z = R(R(res) + D(R(x)))                      (z = R(x) without res and with p == 0)
+ *   y = (z - mean) * rstd * R(gamma) + R(beta),  mean and rstd = 1 / sqrt(var + eps) of each row of z
+ *   x, res  rows x cols; res may be NULL
+ *   gamma, beta  cols values, or NULL (1 and 0)
+ *   z       receives z in the element type of `result` (always rounded: the input of a layer is), or NULL
+ *   y       rows x cols
+ *   mean, rstd  rows values each for the backward pass, or both NULL
+ * cols must be at most 32768, eps >= 0.  rows or cols equal to 0 succeeds.
+ */
+int fmt_layernorm_fwd(int64_t rows, int64_t cols, const void *x, int64_t ldx, const void *res, int64_t ldres,
+                      fmt_dropout_t d, const float *gamma, const float *beta, float eps, void *z, int64_t ldz,
+                      void *y, int64_t ldy, float *mean, float *rstd, int32_t store, int32_t result, fmt_format_t f,
+                      void *stream);
+
+/*
+ * fmt_layernorm_bwd -- gradients of the same.  With xhat = (z - mean) * rstd and g = R(dy) * R(gamma):
+ *   dz = rstd * (g - sum(g) / cols - xhat * sum(g * xhat) / cols)   (also the gradient of res)
+ *   dx = D(dz)                                   (or NULL: not wanted)
+ *   dgamma = sum over rows of R(dy) * xhat,  dbeta = sum over rows of R(dy)   (fp32; or both NULL)
+ *   dy, z   in the element type of `store`; z is what the forward call wrote, or its x if it wrote none
+ * The sums over rows are taken in an order that depends on the sizes and the GPU alone: the same inputs give the same bits.
+ * rows == 0 zero-fills dgamma and dbeta.
+ */
+int fmt_layernorm_bwd(int64_t rows, int64_t cols, const void *dy, int64_t lddy, const void *z, int64_t ldz,
+                      const float *mean, const float *rstd, const float *gamma, fmt_dropout_t d, void *dz, int64_t lddz,
+                      void *dx, int64_t lddx, float *dgamma, float *dbeta, int32_t store, int32_t result,
+                      fmt_format_t f, void *stream);
 
 /*
  * fmt_format_info -- closed-form constants of a format (Sec. III; Table I), computed on

@@ -25,6 +25,7 @@ FMT_NBINS = 64
 EXP_LO_DEFAULT = -48
 CLASS_NAMES = ("total", "zero", "underflow", "denormal", "normal", "overflow", "inf", "nan")
 EXPORTS = ("fmt_quantize", "fmt_quantize_static", "fmt_histogram", "fmt_gemm", "fmt_operand_bytes", "fmt_prepare", "fmt_prepare_pair", "fmt_prepare_pair_batch", "fmt_quantize_prepare_pair_batch", "fmt_gemm_prepared", "fmt_gemm_prepared_batch", "fmt_linear_prepared", "fmt_gemm_fmac8", "fmt_linear", "fmt_pack16", "fmt_unpack16", "fmt_linear_pack16", "fmt_conv2d_fwd", "fmt_conv2d_dgrad", "fmt_conv2d_wgrad", "fmt_dls_init", "fmt_dls_step", "fmt_format_info", "fmt_format_thresholds",
+           "fmt_dropout", "fmt_layernorm_fwd", "fmt_layernorm_bwd",
            "fmt_scratch_bytes", "fmt_release_scratch", "fmt_status_string")
 
 
@@ -69,6 +70,10 @@ class _CDlsState(ctypes.Structure):
 class _COperand(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("bytes", ctypes.c_size_t), ("rows", ctypes.c_int64), ("k", ctypes.c_int64),
                 ("format", _CFormat), ("scheme", ctypes.c_int32)]
+
+
+class _CDropout(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("site", ctypes.c_uint32), ("rng", ctypes.c_void_p)]
 
 
 class FmtError(RuntimeError):
@@ -134,6 +139,13 @@ def _load() -> ctypes.CDLL:
     lib.fmt_dls_init.restype = ctypes.c_int
     lib.fmt_dls_step.argtypes = [vp, i64, _CDlsParams, vp, vp]
     lib.fmt_dls_step.restype = ctypes.c_int
+    f32 = ctypes.c_float
+    lib.fmt_dropout.argtypes = [vp, i64, vp, i64, i64, i64, _CDropout, i32, i32, _CFormat, vp]
+    lib.fmt_dropout.restype = ctypes.c_int
+    lib.fmt_layernorm_fwd.argtypes = [i64, i64, vp, i64, vp, i64, _CDropout, vp, vp, f32, vp, i64, vp, i64, vp, vp, i32, i32, _CFormat, vp]
+    lib.fmt_layernorm_fwd.restype = ctypes.c_int
+    lib.fmt_layernorm_bwd.argtypes = [i64, i64, vp, i64, vp, i64, vp, vp, vp, _CDropout, vp, i64, vp, i64, vp, vp, i32, i32, _CFormat, vp]
+    lib.fmt_layernorm_bwd.restype = ctypes.c_int
     dp, ip = ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32)
     lib.fmt_format_info.argtypes = [_CFormat, dp, dp, dp, ip, ip]
     lib.fmt_format_info.restype = ctypes.c_int
@@ -725,6 +737,145 @@ def dls_state_to_dict(state) -> dict:
     raw = bytes(state.cpu().numpy().tobytes())
     st = _CDlsState.from_buffer_copy(raw)
     return {name: getattr(st, name) for name, _ in _CDlsState._fields_}
+
+
+# Operators beside the products: tensors of fp32 values, or of 16-bit codes (int16 / uint16; float16 is the codes of 1/5/10 and
+# bfloat16 those of 1/8/7).
+_RESULTS = {"f32": 0, "round": 1, "code16": 2}
+_CODE_FORMATS = {torch.float16: (5, 10), torch.bfloat16: (8, 7)}
+
+
+def _elem_store(t, name: str, fmt) -> int:
+    """FMT_STORE_* of a tensor's type."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a tensor on the GPU" % name)
+    if t.dtype == torch.float32:
+        return 0
+    if t.dtype in (torch.int16, torch.uint16):
+        return 1
+    if t.dtype in _CODE_FORMATS:
+        if _CODE_FORMATS[t.dtype] != (int(fmt[0]), int(fmt[1])):
+            raise TypeError("%s is %s, which holds codes of 1/%d/%d, not of 1/%d/%d" % (name, t.dtype, *_CODE_FORMATS[t.dtype], fmt[0], fmt[1]))
+        return 1
+    raise TypeError("%s must be float32, or int16, uint16, float16 or bfloat16 codes" % name)
+
+
+def _elem_result(result, like):
+    """FMT_RESULT_* and the type of the tensors that are written; by default they are stored as the inputs are, rounded."""
+    code = like.dtype != torch.float32
+    if result is None:
+        result = "code16" if code else "round"
+    if result not in _RESULTS:
+        raise ValueError("result must be 'f32', 'round' or 'code16'")
+    return _RESULTS[result], (like.dtype if code else torch.int16) if result == "code16" else torch.float32
+
+
+def _same_kind(t, like, name: str):
+    if not isinstance(t, torch.Tensor) or t.dtype != like.dtype or t.shape != like.shape or t.device != like.device:
+        raise TypeError("%s must have the type, shape and device of the first tensor" % name)
+    return t
+
+
+def _as_rows(t, name: str):
+    """(tensor of rows x last dimension, leading dimension), without a copy."""
+    if t.dim() < 1:
+        raise ValueError("%s must have at least one dimension" % name)
+    cols = t.shape[-1]
+    r = t if t.dim() == 2 else t.reshape(1, cols) if t.dim() == 1 else t.view(-1, cols) if t.numel() else t.reshape(0, max(cols, 1))
+    if r.shape[1] > 1 and r.stride(1) != 1:
+        raise ValueError("%s must have unit stride along its last dimension" % name)
+    return r, (r.stride(0) if r.shape[0] > 1 else max(r.shape[1], 1))
+
+
+def _param(t, name: str, n: int, device):
+    if t is None:
+        return None
+    _dev_f32(t, name)
+    if t.numel() != n or not t.is_contiguous() or t.device != device:
+        raise ValueError("%s must be a contiguous float32 tensor of %d values on the inputs' device" % (name, n))
+    return t.data_ptr()
+
+
+def new_rng(seed: int, step: int = 0, device="cuda"):
+    """State of the counter-based generator of :func:`fmt_dropout`: a GPU tensor {seed, step}.  A program adds 1 to ``rng[1]``
+    (on the stream, so also inside a recorded graph) between steps."""
+    signed = [v - (1 << 64) if v >= 1 << 63 else v for v in (int(seed) % (1 << 64), int(step) % (1 << 64))]
+    return torch.tensor(signed, dtype=torch.int64, device=device)
+
+
+def _dropout_arg(p, site, rng, device) -> _CDropout:
+    if rng is not None and (not isinstance(rng, torch.Tensor) or rng.dtype != torch.int64 or rng.numel() != 2 or not rng.is_contiguous()
+                            or rng.device != device):
+        raise TypeError("rng must be a contiguous int64 tensor of two values on the inputs' device (see new_rng)")
+    if not 0 <= int(site) < 1 << 32:
+        raise ValueError("site must be in [0, 2^32)")
+    return _CDropout(float(p), int(site), None if rng is None else rng.data_ptr())
+
+
+def fmt_dropout(x, p: float, rng, fmt, site: int = 0, result=None, out=None, stream=None):
+    """D(R(x)): dropout with the mask made from a counter (see fmt.h); the backward pass is the same call on the gradient.
+    x: float32, rounded to the format as it is read, or 16-bit codes.  ``result``: 'f32' (unrounded), 'round' or 'code16';
+    by default as x is stored, rounded."""
+    store = _elem_store(x, "x", fmt)
+    rows, ldx = _as_rows(x, "x")
+    res, dtype = _elem_result(result, x)
+    d = _dropout_arg(p, site, rng, x.device)
+    if out is None:
+        out = torch.empty(x.shape, dtype=dtype, device=x.device)
+    if out.dtype != dtype or out.shape != x.shape or out.device != x.device:
+        raise ValueError("out must be a tensor of x's shape and of the type of the result")
+    orows, ldy = _as_rows(out, "out")
+    rc = _lib.fmt_dropout(rows.data_ptr(), ldx, orows.data_ptr(), ldy, rows.shape[0], rows.shape[1], d, store, res, _cfmt(fmt),
+                          _call_stream(stream))
+    _check(rc, "fmt_dropout")
+    return out
+
+
+def fmt_layernorm_fwd(x, gamma, beta, fmt, residual=None, p: float = 0.0, rng=None, site: int = 0, eps: float = 1e-5, result=None,
+                      keep: bool = True, stream=None):
+    """Layer norm over the last dimension of z = R(R(residual) + D(R(x))) (of R(x) without residual and dropout).  Returns
+    (y, z, mean, rstd); z is None where it is R(x): the backward pass then takes x.  ``keep=False`` (inference): z, mean and
+    rstd are not written and come back as None.  x, residual: float32 or 16-bit codes; gamma, beta: float32, or None."""
+    store = _elem_store(x, "x", fmt)
+    rows, ldx = _as_rows(x, "x")
+    n, cols = rows.shape
+    res, dtype = _elem_result(result, x)
+    rp, ldr = None, 0
+    if residual is not None:
+        rr, ldr = _as_rows(_same_kind(residual, x, "residual"), "residual")
+        rp = rr.data_ptr()
+    d = _dropout_arg(p, site, rng, x.device)
+    y = torch.empty(x.shape, dtype=dtype, device=x.device)
+    z = torch.empty_like(y) if keep and (residual is not None or p > 0) else None
+    mean, rstd = torch.empty((2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device) if keep else (None, None)
+    rc = _lib.fmt_layernorm_fwd(n, cols, rows.data_ptr(), ldx, rp, ldr, d, _param(gamma, "gamma", cols, x.device),
+                                _param(beta, "beta", cols, x.device), float(eps), None if z is None else z.data_ptr(), cols, y.data_ptr(),
+                                cols, None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), store, res,
+                                _cfmt(fmt), _call_stream(stream))
+    _check(rc, "fmt_layernorm_fwd")
+    return y, z, mean, rstd
+
+
+def fmt_layernorm_bwd(dy, z, mean, rstd, gamma, fmt, p: float = 0.0, rng=None, site: int = 0, result=None, params: bool = True,
+                      stream=None):
+    """Gradients of :func:`fmt_layernorm_fwd`: returns (dz, dx, dgamma, dbeta); dz is the residual's gradient, dx that of x (the
+    same tensor as dz with p == 0).  ``z``: what the forward call returned, or its x where that was None; dy is stored
+    as z is.  ``params=False``: dgamma and dbeta are not wanted."""
+    store = _elem_store(dy, "dy", fmt)
+    _same_kind(z, dy, "z")
+    (rows, lddy), (zrows, ldz) = _as_rows(dy, "dy"), _as_rows(z, "z")
+    n, cols = rows.shape
+    res, dtype = _elem_result(result, dy)
+    d = _dropout_arg(p, site, rng, dy.device)
+    dz = torch.empty(dy.shape, dtype=dtype, device=dy.device)
+    dx = torch.empty_like(dz) if p > 0 else None
+    dgamma, dbeta = torch.empty((2, cols), dtype=torch.float32, device=dy.device) if params else (None, None)
+    rc = _lib.fmt_layernorm_bwd(n, cols, rows.data_ptr(), lddy, zrows.data_ptr(), ldz, _param(mean, "mean", n, dy.device),
+                                _param(rstd, "rstd", n, dy.device), _param(gamma, "gamma", cols, dy.device), d, dz.data_ptr(), cols,
+                                None if dx is None else dx.data_ptr(), cols, None if dgamma is None else dgamma.data_ptr(),
+                                None if dbeta is None else dbeta.data_ptr(), store, res, _cfmt(fmt), _call_stream(stream))
+    _check(rc, "fmt_layernorm_bwd")
+    return dz, (dz if dx is None else dx), dgamma, dbeta
 
 
 def fmt_format_info(fmt) -> dict:

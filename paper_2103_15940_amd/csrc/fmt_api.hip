@@ -5,6 +5,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <utility>
@@ -696,6 +697,131 @@ int fmt_dls_step(const fmt_hist_t *hists, int64_t count, fmt_dls_params_t prm,
                     prm.interval >= 1 && prm.min_scale > 0.0f && prm.min_scale <= prm.max_scale;
     if (!ok) return FMT_ERR_RANGE;
     return launch_dls_step(hists, count, prm, state, static_cast<hipStream_t>(stream));
+}
+
+// Common to the operators beside the products: format, element types.
+static int check_elems(fmt_format_t f, int32_t store, int32_t result, ElemFormat *e)
+{
+    QuantParams p;
+    const int rc = make_quant_params(f, FMT_EXP_LO_DEFAULT, &p);
+    if (rc != FMT_OK) return rc;
+    if ((store != FMT_STORE_F32 && store != FMT_STORE_CODE16) ||
+        (result != FMT_RESULT_F32 && result != FMT_RESULT_ROUND && result != FMT_RESULT_CODE16))
+        return FMT_ERR_RANGE;
+    if ((store == FMT_STORE_CODE16 || result == FMT_RESULT_CODE16) && !has_code16(f)) return FMT_ERR_FORMAT;
+    *e = make_elem_format(f, p);
+    return FMT_OK;
+}
+
+static int check_dropout(const fmt_dropout_t &d)
+{
+    if (!(d.p >= 0.0f && d.p <= 1.0f)) return FMT_ERR_RANGE;
+    if (d.p > 0.0f && !d.rng) return FMT_ERR_NULL;
+    return aligned(d.rng, 8) ? FMT_OK : FMT_ERR_ALIGN;
+}
+
+static size_t store_size(int32_t store) { return store == FMT_STORE_CODE16 ? 2 : 4; }
+static size_t result_size(int32_t result) { return result == FMT_RESULT_CODE16 ? 2 : 4; }
+
+// A rows x cols matrix of a row-wise operator: shape, pointer, alignment.
+struct Rows {
+    const void *p;
+    int64_t ld;
+    size_t size;
+    size_t bytes(int64_t rows, int64_t cols) const { return size * (size_t)((rows - 1) * ld + cols); }
+};
+
+static int check_rows(const Rows &m, int64_t rows, int64_t cols)
+{
+    if (m.ld < cols || m.ld >= ((int64_t)1 << 31) || (rows > 0 && m.ld > ((int64_t)1 << 40) / rows)) return FMT_ERR_SHAPE;
+    return aligned(m.p, m.size) ? FMT_OK : FMT_ERR_ALIGN;
+}
+
+int fmt_dropout(const void *x, int64_t ldx, void *y, int64_t ldy, int64_t rows, int64_t cols, fmt_dropout_t d, int32_t store,
+                int32_t result, fmt_format_t f, void *stream)
+{
+    ElemFormat e;
+    int rc = check_elems(f, store, result, &e);
+    if (rc != FMT_OK) return rc;
+    if (rows < 0 || cols < 0 || cols >= ((int64_t)1 << 31)) return FMT_ERR_SHAPE;
+    if (!(d.p >= 0.0f && d.p <= 1.0f)) return FMT_ERR_RANGE;
+    if (rows == 0 || cols == 0) return FMT_OK;
+    if (!x || !y || !d.rng) return FMT_ERR_NULL;
+    if (!aligned(d.rng, 8)) return FMT_ERR_ALIGN;
+    const Rows in{x, ldx, store_size(store)}, out{y, ldy, result_size(result)};
+    if ((rc = check_rows(in, rows, cols)) != FMT_OK || (rc = check_rows(out, rows, cols)) != FMT_OK) return rc;
+    const bool in_place = x == y && ldx == ldy && in.size == out.size;       // an element is read and written by one thread
+    if ((!in_place && overlap(x, in.bytes(rows, cols), y, out.bytes(rows, cols))) || overlap(d.rng, 16, y, out.bytes(rows, cols)))
+        return FMT_ERR_ALIAS;
+    return launch_dropout(x, ldx, y, ldy, rows, cols, d, store, result, e, static_cast<hipStream_t>(stream));
+}
+
+// Spans of memory of one call; whether one that is written lies over any other.
+struct Span {
+    const void *p;
+    size_t bytes;
+    bool written;
+};
+static bool clash(std::initializer_list<Span> spans)
+{
+    for (const Span &s : spans)
+        for (const Span &t : spans)
+            if (&s != &t && s.written && s.p && t.p && overlap(s.p, s.bytes, t.p, t.bytes)) return true;
+    return false;
+}
+
+int fmt_layernorm_fwd(int64_t rows, int64_t cols, const void *x, int64_t ldx, const void *res, int64_t ldres, fmt_dropout_t d,
+                      const float *gamma, const float *beta, float eps, void *z, int64_t ldz, void *y, int64_t ldy, float *mean,
+                      float *rstd, int32_t store, int32_t result, fmt_format_t f, void *stream)
+{
+    ElemFormat e;
+    int rc = check_elems(f, store, result, &e);
+    if (rc != FMT_OK) return rc;
+    if (rows < 0 || cols < 0 || cols > kNormMaxCols) return FMT_ERR_SHAPE;
+    if (!(eps >= 0.0f)) return FMT_ERR_RANGE;
+    if ((rc = check_dropout(d)) != FMT_OK) return rc;
+    if (rows == 0 || cols == 0) return FMT_OK;
+    if (!x || !y || (!mean) != (!rstd)) return FMT_ERR_NULL;
+    const size_t si = store_size(store), so = result_size(result);
+    const Rows m[4] = {{x, ldx, si}, {y, ldy, so}, {res, res ? ldres : cols, si}, {z, z ? ldz : cols, so}};
+    for (const Rows &r : m)
+        if ((rc = check_rows(r, rows, cols)) != FMT_OK) return rc;
+    if (!aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return FMT_ERR_ALIGN;
+    const size_t nw = 4 * (size_t)cols, nr = 4 * (size_t)rows;
+    const std::initializer_list<Span> spans = {{x, m[0].bytes(rows, cols), false},   {res, m[2].bytes(rows, cols), false}, {gamma, nw, false},
+                          {beta, nw, false},                    {d.p > 0.0f ? d.rng : nullptr, 16, false}, {y, m[1].bytes(rows, cols), true},
+                          {z, m[3].bytes(rows, cols), true},    {mean, nr, true},                     {rstd, nr, true}};
+    if (clash(spans)) return FMT_ERR_ALIAS;
+    return launch_layernorm_fwd(LayerNorm{rows, cols, d, store, result}, x, ldx, res, ldres, gamma, beta, eps, z, ldz, y, ldy, mean,
+                                rstd, e, static_cast<hipStream_t>(stream));
+}
+
+int fmt_layernorm_bwd(int64_t rows, int64_t cols, const void *dy, int64_t lddy, const void *z, int64_t ldz, const float *mean,
+                      const float *rstd, const float *gamma, fmt_dropout_t d, void *dz, int64_t lddz, void *dx, int64_t lddx,
+                      float *dgamma, float *dbeta, int32_t store, int32_t result, fmt_format_t f, void *stream)
+{
+    ElemFormat e;
+    int rc = check_elems(f, store, result, &e);
+    if (rc != FMT_OK) return rc;
+    if (rows < 0 || cols < 0 || cols > kNormMaxCols) return FMT_ERR_SHAPE;
+    if ((rc = check_dropout(d)) != FMT_OK) return rc;
+    if (cols == 0) return FMT_OK;
+    if ((!dgamma) != (!dbeta)) return FMT_ERR_NULL;
+    if (rows > 0 && (!dy || !z || !mean || !rstd || !dz)) return FMT_ERR_NULL;
+    const size_t si = store_size(store), so = result_size(result);
+    const Rows m[4] = {{dy, lddy, si}, {z, ldz, si}, {dz, lddz, so}, {dx, dx ? lddx : cols, so}};
+    if (rows > 0)
+        for (const Rows &r : m)
+            if ((rc = check_rows(r, rows, cols)) != FMT_OK) return rc;
+    if (!aligned(gamma, 4) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4)) return FMT_ERR_ALIGN;
+    const size_t nw = 4 * (size_t)cols, nr = 4 * (size_t)rows;
+    auto mat = [&](int i, bool written) { return Span{rows > 0 ? m[i].p : nullptr, rows > 0 ? m[i].bytes(rows, cols) : 0, written}; };
+    const std::initializer_list<Span> spans = {mat(0, false), mat(1, false), {mean, nr, false}, {rstd, nr, false}, {gamma, nw, false},
+                          {d.p > 0.0f ? d.rng : nullptr, 16, false}, mat(2, true), mat(3, true), {dgamma, nw, true}, {dbeta, nw, true}};
+    if (clash(spans)) return FMT_ERR_ALIAS;
+    if (rows == 0 && !dgamma) return FMT_OK;
+    return launch_layernorm_bwd(LayerNorm{rows, cols, d, store, result}, dy, lddy, z, ldz, mean, rstd, gamma, dz, lddz, dx, lddx, dgamma,
+                                dbeta, e, static_cast<hipStream_t>(stream));
 }
 
 int fmt_format_info(fmt_format_t f, double *maxN, double *minN, double *minD,

@@ -158,6 +158,44 @@ int launch_dls_init(fmt_dls_state_t *state, float loss_scale, hipStream_t stream
 int launch_dls_step(const fmt_hist_t *hists, int64_t count, fmt_dls_params_t prm, fmt_dls_state_t *state,
                     hipStream_t stream);
 
+// How codes and fp32 are turned into each other (uniform per launch, from the format).
+enum : int {
+    kCodecGeneric = 0,  // decode_bits / encode_bits
+    kCodecBf16 = 1,     // 1/8/7: the upper half of the fp32 pattern
+    kCodecHalf = 2,     // 1/5/10 with denormals: the conversions of the vector units
+    kCodecNone = 3      // 1/8/23 with denormals: every fp32 value is the format's
+};
+
+struct ElemFormat {
+    QuantParams p;
+    int32_t ftz, codec;
+};
+
+inline ElemFormat make_elem_format(fmt_format_t f, const QuantParams &p)
+{
+    const int codec = f.e == 8 && f.m == 7                   ? kCodecBf16
+                      : f.e == 5 && f.m == 10 && f.denorm != 0 ? kCodecHalf
+                      : f.e == 8 && f.m == 23 && f.denorm != 0 ? kCodecNone
+                                                               : kCodecGeneric;
+    return ElemFormat{p, f.denorm == 0, codec};
+}
+
+// Row-wise operators (fmt_norm.hip).
+struct LayerNorm {
+    int64_t rows, cols;
+    fmt_dropout_t drop;
+    int32_t store, result;      // FMT_STORE_*, FMT_RESULT_*
+};
+constexpr int64_t kNormMaxCols = 32768;
+int launch_dropout(const void *x, int64_t ldx, void *y, int64_t ldy, int64_t rows, int64_t cols, const fmt_dropout_t &d, int32_t store,
+                   int32_t result, const ElemFormat &f, hipStream_t stream);
+int launch_layernorm_fwd(const LayerNorm &n, const void *x, int64_t ldx, const void *res, int64_t ldres, const float *gamma,
+                         const float *beta, float eps, void *z, int64_t ldz, void *y, int64_t ldy, float *mean, float *rstd,
+                         const ElemFormat &f, hipStream_t stream);
+int launch_layernorm_bwd(const LayerNorm &n, const void *dy, int64_t lddy, const void *z, int64_t ldz, const float *mean,
+                         const float *rstd, const float *gamma, void *dz, int64_t lddz, void *dx, int64_t lddx, float *dgamma,
+                         float *dbeta, const ElemFormat &f, hipStream_t stream);
+
 // Reports a failed HIP call on stderr when the environment variable FMT_VERBOSE is set.
 void report_hip_error(const char *expr, const char *file, int line, hipError_t err);
 

@@ -592,6 +592,56 @@ int fmt_layernorm_bwd(int64_t rows, int64_t cols, const void *dy, int64_t lddy, 
                       fmt_format_t f, void *stream);
 
 /*
+ * Attention of `heads` query heads over `kv_heads` heads of keys and values (heads a multiple of kv_heads; query head h
+ * reads kv head h / (heads / kv_heads)), with an optional sliding window and a few first tokens that stay visible (sinks).
+ *
+ *   S = scale * R(Q) R(K)^T over the visible keys,  lse = log sum exp S of a row,  O = exp(S - lse) R(V)
+ *
+ * Sequence b has length = k_lens[b] keys (k_lens NULL: k_len; values outside [0, k_len] are clamped), and its query i stands
+ * at position pos = q_pos[b] + i (q_pos NULL: k_len - q_len + i: the queries are the last tokens).  Key j is visible if
+ *   j < length,  and j <= pos if causal,  and |pos - j| < window or j < sinks if window > 0.
+ * A row that sees no key gives O = 0 and lse = -infinity, and zero gradients.  Keys and values from `length` on are never
+ * looked at, whatever they hold; infinities and NaN in keys or values before it may make NaN of any row of their heads
+ * that shares a tile with them.
+ *
+ * Tensors are [batch][token][head][dim] with any strides along the first three (in elements, not negative; inputs may have
+ * strides of 0) and unit stride along dim: parts of a fused projection, a cache with room to grow.  1 <= dim <= 128.
+ * Formats of at most 15 stored mantissa bits (FMT_ERR_FORMAT otherwise; e == 8 with m >= 8: see fmt_gemm about values
+ * below 2^(m-133)).  Products of operands are exact and added in fp32; P = exp(S - lse) and dS are held to 24 bits where the
+ * result is FMT_RESULT_F32, and to 16 (8 for m <= 7) where it is rounded to the format anyway; P below 2^-126 is 0.
+ * Sums are taken in an order that depends on the sizes and the GPU alone.
+ */
+typedef struct fmt_attention {
+    int32_t batch, heads, kv_heads, q_len, k_len, dim;
+    int32_t causal;        /* 0 or 1 */
+    int32_t window, sinks; /* 0 <= window, sinks < 2^30; window == 0: no window */
+    float scale;           /* finite */
+    const int32_t *k_lens; /* device, batch values, or NULL */
+    const int32_t *q_pos;  /* device, batch values in (-2^30, 2^30), or NULL */
+} fmt_attention_t;
+
+typedef struct fmt_view {
+    void *data;            /* device */
+    int64_t stride_b, stride_t, stride_h;
+} fmt_view_t;
+
+/* lse: [batch][heads][q_len] fp32, or NULL (inference). */
+int fmt_attention_fwd(fmt_attention_t a, fmt_view_t q, fmt_view_t k, fmt_view_t v, fmt_view_t o, float *lse,
+                      int32_t store, int32_t result, fmt_format_t f, void *stream);
+
+/*
+ * Gradients of the same:
+ *   P = exp(S - lse),  delta = sum over dim of R(dO) * O,  dS = P * (R(dO) R(V)^T - delta),
+ *   dQ = scale * dS R(K),  dK = scale * dS^T R(Q),  dV = P^T R(dO)   (dK and dV: sums over the query heads that share them)
+ *   o, lse   what the forward call gave; o, d_o, dq, dk and dv are stored as `result` says (codes, or fp32; d_o in fp32 is
+ *            rounded as it is read, o is not), q, k, v as `store` says
+ * dk and dv are [batch][k_len][kv_heads][dim]; rows from `length` on are zero.
+ */
+int fmt_attention_bwd(fmt_attention_t a, fmt_view_t q, fmt_view_t k, fmt_view_t v, fmt_view_t o, fmt_view_t d_o,
+                      const float *lse, fmt_view_t dq, fmt_view_t dk, fmt_view_t dv, int32_t store, int32_t result,
+                      fmt_format_t f, void *stream);
+
+/*
  * fmt_format_info -- closed-form constants of a format (Sec. III; Table I), computed on
  * the host.  Any output pointer may be NULL.  Returns FMT_ERR_FORMAT for an unsupported
  * format.

@@ -25,7 +25,7 @@ FMT_NBINS = 64
 EXP_LO_DEFAULT = -48
 CLASS_NAMES = ("total", "zero", "underflow", "denormal", "normal", "overflow", "inf", "nan")
 EXPORTS = ("fmt_quantize", "fmt_quantize_static", "fmt_histogram", "fmt_gemm", "fmt_operand_bytes", "fmt_prepare", "fmt_prepare_pair", "fmt_prepare_pair_batch", "fmt_quantize_prepare_pair_batch", "fmt_gemm_prepared", "fmt_gemm_prepared_batch", "fmt_linear_prepared", "fmt_gemm_fmac8", "fmt_linear", "fmt_pack16", "fmt_unpack16", "fmt_linear_pack16", "fmt_conv2d_fwd", "fmt_conv2d_dgrad", "fmt_conv2d_wgrad", "fmt_dls_init", "fmt_dls_step", "fmt_format_info", "fmt_format_thresholds",
-           "fmt_dropout", "fmt_layernorm_fwd", "fmt_layernorm_bwd",
+           "fmt_dropout", "fmt_layernorm_fwd", "fmt_layernorm_bwd", "fmt_attention_fwd", "fmt_attention_bwd",
            "fmt_scratch_bytes", "fmt_release_scratch", "fmt_status_string")
 
 
@@ -74,6 +74,15 @@ class _COperand(ctypes.Structure):
 
 class _CDropout(ctypes.Structure):
     _fields_ = [("p", ctypes.c_float), ("site", ctypes.c_uint32), ("rng", ctypes.c_void_p)]
+
+
+class _CAttention(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("batch", "heads", "kv_heads", "q_len", "k_len", "dim", "causal", "window", "sinks")] + [
+        ("scale", ctypes.c_float), ("k_lens", ctypes.c_void_p), ("q_pos", ctypes.c_void_p)]
+
+
+class _CView(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
 
 
 class FmtError(RuntimeError):
@@ -146,6 +155,10 @@ def _load() -> ctypes.CDLL:
     lib.fmt_layernorm_fwd.restype = ctypes.c_int
     lib.fmt_layernorm_bwd.argtypes = [i64, i64, vp, i64, vp, i64, vp, vp, vp, _CDropout, vp, i64, vp, i64, vp, vp, i32, i32, _CFormat, vp]
     lib.fmt_layernorm_bwd.restype = ctypes.c_int
+    lib.fmt_attention_fwd.argtypes = [_CAttention] + [_CView] * 4 + [vp, i32, i32, _CFormat, vp]
+    lib.fmt_attention_fwd.restype = ctypes.c_int
+    lib.fmt_attention_bwd.argtypes = [_CAttention] + [_CView] * 5 + [vp] + [_CView] * 3 + [i32, i32, _CFormat, vp]
+    lib.fmt_attention_bwd.restype = ctypes.c_int
     dp, ip = ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32)
     lib.fmt_format_info.argtypes = [_CFormat, dp, dp, dp, ip, ip]
     lib.fmt_format_info.restype = ctypes.c_int
@@ -876,6 +889,73 @@ def fmt_layernorm_bwd(dy, z, mean, rstd, gamma, fmt, p: float = 0.0, rng=None, s
                                 None if dbeta is None else dbeta.data_ptr(), store, res, _cfmt(fmt), _call_stream(stream))
     _check(rc, "fmt_layernorm_bwd")
     return dz, (dz if dx is None else dx), dgamma, dbeta
+
+
+def _view4(t, name: str) -> _CView:
+    """[batch, token, head, dim] with unit stride along dim."""
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError("%s must be [batch, token, head, dim] with unit stride along dim" % name)
+    return _CView(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+
+def _per_sequence(t, name: str, batch: int, device):
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.numel() != batch or not t.is_contiguous() or t.device != device:
+        raise TypeError("%s must be a contiguous int32 tensor with one value per sequence, on the inputs' device" % name)
+    return t.data_ptr()
+
+
+def _attention_args(q, k, v, fmt, causal, window, sinks, scale, k_lens, q_pos):
+    """(FMT_STORE_*, fmt_attention_t, views of q, k and v)."""
+    store = _elem_store(q, "q", fmt)
+    views = _view4(q, "q"), _view4(k, "k"), _view4(v, "v")
+    b, nq, h, d = q.shape
+    if k.dtype != q.dtype or v.dtype != q.dtype or k.device != q.device or v.device != q.device:
+        raise TypeError("k and v must have the type and device of q")
+    if k.shape != v.shape or k.shape[0] != b or k.shape[3] != d:
+        raise ValueError("k and v must be [batch, tokens, kv heads, dim] with q's batch and dim")
+    if not (0 <= int(window) < 1 << 30 and 0 <= int(sinks) < 1 << 30):
+        raise ValueError("window and sinks must be in [0, 2^30)")
+    a = _CAttention(b, h, k.shape[2], nq, k.shape[1], d, 1 if causal else 0, int(window), int(sinks),
+                    d ** -0.5 if scale is None else float(scale), _per_sequence(k_lens, "k_lens", b, q.device),
+                    _per_sequence(q_pos, "q_pos", b, q.device))
+    return store, a, views
+
+
+def fmt_attention_fwd(q, k, v, fmt, causal: bool = False, window: int = 0, sinks: int = 0, scale: Optional[float] = None, k_lens=None,
+                      q_pos=None, result=None, keep: bool = True, stream=None):
+    """softmax(scale R(q) R(k)^T) R(v) over the visible keys (see fmt.h).  q: [batch, q tokens, heads, dim]; k, v: [batch, k tokens, kv
+    heads, dim], float32 or 16-bit codes, any strides but a unit one along dim.  ``window`` > 0: the keys less than so many tokens away,
+    and the first ``sinks``; ``k_lens``: int32 lengths of the sequences; ``q_pos``: int32 positions of their first queries (by
+    default the queries are the last tokens); ``scale``: by default dim ** -0.5.  Returns (o, lse); ``keep=False`` (inference): lse is
+    None."""
+    store, a, views = _attention_args(q, k, v, fmt, causal, window, sinks, scale, k_lens, q_pos)
+    res, dtype = _elem_result(result, q)
+    o = torch.empty(q.shape, dtype=dtype, device=q.device)
+    lse = torch.empty((a.batch, a.heads, a.q_len), dtype=torch.float32, device=q.device) if keep else None
+    rc = _lib.fmt_attention_fwd(a, *views, _view4(o, "o"), None if lse is None else lse.data_ptr(), store, res, _cfmt(fmt),
+                                _call_stream(stream))
+    _check(rc, "fmt_attention_fwd")
+    return o, lse
+
+
+def fmt_attention_bwd(d_o, q, k, v, o, lse, fmt, causal: bool = False, window: int = 0, sinks: int = 0, scale: Optional[float] = None,
+                      k_lens=None, q_pos=None, result=None, stream=None):
+    """Gradients (dq, dk, dv) of :func:`fmt_attention_fwd`, called with the same arguments; d_o is stored as o is."""
+    store, a, views = _attention_args(q, k, v, fmt, causal, window, sinks, scale, k_lens, q_pos)
+    res, dtype = _elem_result(result, q)
+    for t, name in ((d_o, "d_o"), (o, "o")):
+        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != q.shape or t.device != q.device:
+            raise TypeError("%s must have q's shape and the type of the result" % name)
+    if not isinstance(lse, torch.Tensor) or lse.dtype != torch.float32 or tuple(lse.shape) != (a.batch, a.heads, a.q_len) \
+            or not lse.is_contiguous() or lse.device != q.device:
+        raise TypeError("lse must be what fmt_attention_fwd returned")
+    dq, dk, dv = (torch.empty(t.shape, dtype=dtype, device=q.device) for t in (q, k, v))
+    rc = _lib.fmt_attention_bwd(a, *views, _view4(o, "o"), _view4(d_o, "d_o"), lse.data_ptr(), _view4(dq, "dq"), _view4(dk, "dk"),
+                                _view4(dv, "dv"), store, res, _cfmt(fmt), _call_stream(stream))
+    _check(rc, "fmt_attention_bwd")
+    return dq, dk, dv
 
 
 def fmt_format_info(fmt) -> dict:

@@ -1,5 +1,6 @@
 // C-ABI entry points of libfmt: argument validation, format constants, scratch management.
 // The arithmetic lives in fmt_stream.hip (quantize / histogram) and fmt_gemm.hip.
+#include <algorithm>
 #include <vector>
 #include <cmath>
 #include <cstdio>
@@ -822,6 +823,133 @@ int fmt_layernorm_bwd(int64_t rows, int64_t cols, const void *dy, int64_t lddy, 
     if (rows == 0 && !dgamma) return FMT_OK;
     return launch_layernorm_bwd(LayerNorm{rows, cols, d, store, result}, dy, lddy, z, ldz, mean, rstd, gamma, dz, lddz, dx, lddx, dgamma,
                                 dbeta, e, static_cast<hipStream_t>(stream));
+}
+
+// A [batch][tokens][heads][dim] tensor of an attention call.
+struct AttnTensor {
+    fmt_view_t v;
+    int64_t tokens, heads;
+    size_t size;
+    bool written;
+    bool empty(const fmt_attention_t &a) const { return a.batch == 0 || tokens == 0 || heads == 0; }
+    int64_t extent(const fmt_attention_t &a) const      // elements from the first to past the last
+    {
+        return (a.batch - 1) * v.stride_b + (tokens - 1) * v.stride_t + (heads - 1) * v.stride_h + a.dim;
+    }
+};
+
+static int check_attn_tensor(const AttnTensor &t, const fmt_attention_t &a)
+{
+    if (t.empty(a)) return FMT_OK;
+    const int64_t n[3] = {a.batch, t.tokens, t.heads};
+    int64_t stride[3] = {t.v.stride_b, t.v.stride_t, t.v.stride_h};
+    for (int i = 0; i < 3; ++i)
+        if (stride[i] < 0 || (n[i] > 1 && stride[i] > ((int64_t)1 << 40) / n[i])) return FMT_ERR_SHAPE;
+    for (int i = 0; i < 3; ++i)
+        if (n[i] <= 1) stride[i] = 0;
+    if (t.written) {                     // no two of its elements may be one: from the smallest stride up, each spans what is inside it
+        int order[3] = {0, 1, 2};
+        for (int i = 0; i < 3; ++i)
+            for (int j = i + 1; j < 3; ++j)
+                if (stride[order[j]] < stride[order[i]]) std::swap(order[i], order[j]);
+        int64_t inside = a.dim;
+        for (int i : order)
+            if (n[i] > 1) {
+                if (stride[i] < inside) return FMT_ERR_SHAPE;
+                inside = stride[i] * (n[i] - 1) + inside;
+            }
+    }
+    if (!t.v.data) return FMT_ERR_NULL;
+    return aligned(t.v.data, t.size) ? FMT_OK : FMT_ERR_ALIGN;
+}
+
+// Whether two tensors share an element: their spans meet, and they are not slices side by side of the tokens of one tensor.
+static bool attn_clash(const AttnTensor &s, const AttnTensor &t, const fmt_attention_t &a)
+{
+    if (s.empty(a) || t.empty(a)) return false;
+    if (!overlap(s.v.data, s.size * (size_t)s.extent(a), t.v.data, t.size * (size_t)t.extent(a))) return false;
+    const bool alike = s.size == t.size && s.v.stride_t == t.v.stride_t && (a.batch == 1 || s.v.stride_b == t.v.stride_b);
+    const int64_t size = (int64_t)s.size, row = size * s.v.stride_t;
+    const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(t.v.data) - reinterpret_cast<uintptr_t>(s.v.data));
+    const int64_t swide = size * ((s.heads - 1) * s.v.stride_h + a.dim), twide = size * ((t.heads - 1) * t.v.stride_h + a.dim);
+    const bool batches_apart = a.batch == 1 || s.v.stride_b >= std::max(s.tokens, t.tokens) * s.v.stride_t;
+    return !(alike && batches_apart && (apart >= 0 ? apart >= swide && apart + twide <= row : -apart >= twide && -apart + swide <= row));
+}
+
+// What both directions check; *e and *s are filled.
+static int check_attention(const fmt_attention_t &a, std::initializer_list<AttnTensor> tensors, std::initializer_list<Span> spans,
+                           int32_t store, int32_t result, fmt_format_t f, ElemFormat *e, AttnShape *s)
+{
+    int rc = check_elems(f, store, result, e);
+    if (rc != FMT_OK) return rc;
+    if (f.m > 15) return FMT_ERR_FORMAT;
+    const int32_t lim = 1 << 30;
+    if (a.batch < 0 || a.heads < 0 || a.q_len < 0 || a.k_len < 0 || a.kv_heads < 1 || a.dim < 1 || a.dim > kAttnMaxDim) return FMT_ERR_SHAPE;
+    if (a.batch > 65535 || a.kv_heads > 65535 || a.heads % a.kv_heads != 0 || a.q_len >= lim || a.k_len >= lim) return FMT_ERR_SHAPE;
+    if ((int64_t)a.q_len * std::max(a.heads / a.kv_heads, 1) >= lim || (int64_t)a.batch * a.heads > ((int64_t)1 << 40) / std::max(a.q_len, 1))
+        return FMT_ERR_SHAPE;
+    if ((a.causal != 0 && a.causal != 1) || a.window < 0 || a.window >= lim || a.sinks < 0 || a.sinks >= lim || !std::isfinite(a.scale))
+        return FMT_ERR_RANGE;
+    for (const AttnTensor &t : tensors)
+        if ((rc = check_attn_tensor(t, a)) != FMT_OK) return rc;
+    if (!aligned(a.k_lens, 4) || !aligned(a.q_pos, 4)) return FMT_ERR_ALIGN;
+    for (const Span &p : spans)
+        if (!aligned(p.p, 4)) return FMT_ERR_ALIGN;
+    for (const AttnTensor &t : tensors) {
+        if (!t.written) continue;
+        for (const AttnTensor &o : tensors)
+            if (&o != &t && attn_clash(t, o, a)) return FMT_ERR_ALIAS;
+        if (t.empty(a)) continue;
+        const size_t bytes = t.size * (size_t)t.extent(a), n = 4 * (size_t)a.batch;
+        if ((a.k_lens && overlap(t.v.data, bytes, a.k_lens, n)) || (a.q_pos && overlap(t.v.data, bytes, a.q_pos, n))) return FMT_ERR_ALIAS;
+        for (const Span &p : spans)
+            if (p.p && overlap(t.v.data, bytes, p.p, p.bytes)) return FMT_ERR_ALIAS;
+    }
+    for (const Span &p : spans) {
+        if (!p.written || !p.p) continue;
+        for (const AttnTensor &t : tensors)
+            if (!t.empty(a) && overlap(p.p, p.bytes, t.v.data, t.size * (size_t)t.extent(a))) return FMT_ERR_ALIAS;
+        if ((a.k_lens && overlap(p.p, p.bytes, a.k_lens, 4 * (size_t)a.batch)) || (a.q_pos && overlap(p.p, p.bytes, a.q_pos, 4 * (size_t)a.batch)))
+            return FMT_ERR_ALIAS;
+    }
+    *s = AttnShape{a.batch, a.heads, a.kv_heads, a.heads / a.kv_heads, a.q_len, a.k_len, a.dim, a.causal, a.window, a.sinks, a.scale,
+                   static_cast<float>(static_cast<double>(a.scale) * 1.4426950408889634), a.k_lens, a.q_pos};
+    return FMT_OK;
+}
+
+static AttnView attn_view(const fmt_view_t &v) { return AttnView{v.data, v.stride_b, v.stride_t, v.stride_h}; }
+
+int fmt_attention_fwd(fmt_attention_t a, fmt_view_t q, fmt_view_t k, fmt_view_t v, fmt_view_t o, float *lse, int32_t store,
+                      int32_t result, fmt_format_t f, void *stream)
+{
+    ElemFormat e;
+    AttnShape s;
+    const size_t si = store_size(store), so = result_size(result);
+    const int rc = check_attention(a, {{q, a.q_len, a.heads, si, false}, {k, a.k_len, a.kv_heads, si, false},
+                                       {v, a.k_len, a.kv_heads, si, false}, {o, a.q_len, a.heads, so, true}},
+                                   {{lse, 4 * (size_t)a.batch * (size_t)a.heads * (size_t)a.q_len, true}}, store, result, f, &e, &s);
+    if (rc != FMT_OK) return rc;
+    if (a.batch == 0 || a.heads == 0 || a.q_len == 0) return FMT_OK;
+    return launch_attention_fwd(s, attn_view(q), attn_view(k), attn_view(v), attn_view(o), lse, store, result, e, f.m,
+                                static_cast<hipStream_t>(stream));
+}
+
+int fmt_attention_bwd(fmt_attention_t a, fmt_view_t q, fmt_view_t k, fmt_view_t v, fmt_view_t o, fmt_view_t d_o, const float *lse,
+                      fmt_view_t dq, fmt_view_t dk, fmt_view_t dv, int32_t store, int32_t result, fmt_format_t f, void *stream)
+{
+    ElemFormat e;
+    AttnShape s;
+    const size_t si = store_size(store), so = result_size(result);
+    const int rc = check_attention(a, {{q, a.q_len, a.heads, si, false}, {k, a.k_len, a.kv_heads, si, false},
+                                       {v, a.k_len, a.kv_heads, si, false}, {o, a.q_len, a.heads, so, false},
+                                       {d_o, a.q_len, a.heads, so, false}, {dq, a.q_len, a.heads, so, true},
+                                       {dk, a.k_len, a.kv_heads, so, true}, {dv, a.k_len, a.kv_heads, so, true}},
+                                   {{lse, 4 * (size_t)a.batch * (size_t)a.heads * (size_t)a.q_len, false}}, store, result, f, &e, &s);
+    if (rc != FMT_OK) return rc;
+    if (a.batch == 0 || (a.heads == 0 && a.k_len == 0) || (a.q_len == 0 && a.k_len == 0)) return FMT_OK;
+    if (!lse && a.heads > 0 && a.q_len > 0) return FMT_ERR_NULL;
+    return launch_attention_bwd(s, attn_view(q), attn_view(k), attn_view(v), attn_view(o), attn_view(d_o), lse, attn_view(dq), attn_view(dk),
+                                attn_view(dv), store, result, e, f.m, static_cast<hipStream_t>(stream));
 }
 
 int fmt_format_info(fmt_format_t f, double *maxN, double *minN, double *minD,

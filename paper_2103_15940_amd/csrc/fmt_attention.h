@@ -1,0 +1,255 @@
+// Attention on the matrix cores: what its kernels share.
+//
+//   S = scale R(Q) R(K)^T, visible pairs only;  P = exp(S - lse), lse = log sum exp S of a row;  O = P R(V)
+//   delta = sum R(dO) O;  dP = R(dO) R(V)^T;  dS = P (dP - delta);
+//   dQ = scale dS R(K);  dK = scale dS^T R(Q);  dV = P^T R(dO)
+//
+// Key j is visible to the query at position i where j < length, j <= i (causal), and |i - j| < window or j < sinks (window > 0).
+//
+// Heads that share keys and values are taken as rows of one product: row r is query r / group of head r % group of the group, so a
+// tile of keys is read once for all of them, and gradients of shared keys and values add up in the accumulators.
+//
+// Operands are split exactly into NQ bf16 pieces (1: 1/8/7 and narrower, 2: up to 16 significant bits), whose products are exact in
+// the matrix cores and added in fp32.  P and dS, which are fp32, go in NP pieces: 3 hold all of their 24 bits (results in
+// unrounded fp32), 1 or 2 hold as many as the operands have (results that are rounded to the format).  Products of pieces that lie
+// below 2^-24 of the largest are left out.
+//
+// Layout of v_mfma_f32_32x32x16: A gives lane l row l % 32 and the 8 k from 8 (l / 32); B the same with columns; the result gives lane l column
+// l % 32, and its register i row 8 (i / 4) + 4 (l / 32) + i % 4.  So registers 8b to 8b + 7 of a result are, as they stand, a B operand for
+// the 16 k from 16b, in an order of k that its A operand has to follow: the lower lanes have k 0-3 and 8-11, the upper 4-7 and 12-15.  P and
+// dS thus go from one product into the next without leaving their lanes; the A operand with that order, and transposed, comes out of LDS
+// with ds_read_b64_tr_b16 (16 lanes read 4 rows x 16 columns, lane i receives column i).
+#pragma once
+
+#include <type_traits>
+
+#include "fmt_elem.h"
+
+namespace fmt {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct AttnSeq {              // one sequence's length and the position of its first query
+    int length, first;
+};
+
+__device__ __forceinline__ AttnSeq attn_seq(const AttnShape &s, int b)
+{
+    int length = s.k_len, first = s.k_len - s.q_len;
+    if (s.k_lens) length = min(max(s.k_lens[b], 0), s.k_len);
+    if (s.q_pos) first = min(max(s.q_pos[b], -(1 << 30)), 1 << 30);
+    return AttnSeq{length, first};
+}
+
+// Whether key j < length is visible from position i.
+__device__ __forceinline__ bool attn_sees(const AttnShape &s, int length, int i, int j)
+{
+    const int d = i - j;
+    const bool near = s.window == 0 || (d < s.window && d > -s.window) || j < s.sinks;
+    return j < length && (!s.causal || d >= 0) && near;
+}
+
+// Whether every key of [k0, k1) is visible from every position of [i0, i1].
+__device__ __forceinline__ bool attn_sees_all(const AttnShape &s, int length, int64_t i0, int64_t i1, int k0, int k1)
+{
+    const bool near = s.window == 0 || k1 <= s.sinks || (i1 - k0 < s.window && k1 - 1 - i0 < s.window);
+    return k1 <= length && (!s.causal || k1 - 1 <= i0) && near;
+}
+
+// Keys that positions [i0, i1] may see: tiles of `tile` keys, [0, sinks) and [first, last).
+struct AttnTiles {
+    int sinks, first, last;
+    __device__ int count() const { return sinks + max(0, last - first); }
+    __device__ int at(int n) const { return n < sinks ? n : first + (n - sinks); }
+};
+
+__device__ __forceinline__ AttnTiles attn_tiles(const AttnShape &s, int length, int64_t i0, int64_t i1, int tile)
+{
+    int64_t end = length, begin = 0, sinks = 0;
+    if (s.causal) end = min(end, i1 + 1);
+    if (s.window) {
+        sinks = min(static_cast<int64_t>(s.sinks), end);
+        begin = max(static_cast<int64_t>(0), i0 - s.window + 1);
+        end = min(end, i1 + s.window);
+    }
+    AttnTiles t;
+    t.sinks = sinks > 0 ? static_cast<int>((sinks + tile - 1) / tile) : 0;
+    t.first = max(static_cast<int>(min(begin, static_cast<int64_t>(length)) / tile), t.sinks);
+    t.last = end > 0 ? static_cast<int>((end + tile - 1) / tile) : 0;
+    return t;
+}
+
+// The upper halves of two fp32 patterns in one register.
+__device__ __forceinline__ uint32_t upper_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+
+// Eight fp32 values as N bf16 pieces whose sum they are (N == 1: to nearest; a last piece that cannot hold the rest: to nearest).
+template <int N>
+__device__ __forceinline__ void bf16_pieces(const float (&v)[8], u32x4 (&out)[N])
+{
+    float rest[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = v[i];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        if (n == N - 1) {
+            bf16x8 last;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) last[i] = static_cast<__bf16>(rest[i]);
+            out[n] = __builtin_bit_cast(u32x4, last);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const uint32_t a = __float_as_uint(rest[i]), b = __float_as_uint(rest[i + 1]);
+                out[n][i / 2] = upper_halves(a, b);
+                rest[i] = __fsub_rn(rest[i], __uint_as_float(a & 0xFFFF0000u));
+                rest[i + 1] = __fsub_rn(rest[i + 1], __uint_as_float(b & 0xFFFF0000u));
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ f32x16 mfma_bf16(u32x4 a, u32x4 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// acc += A B over all pairs of pieces that count: NA + NB - 2 is the last order that three pieces of one side leave (24 bits).
+template <int NA, int NB>
+__device__ __forceinline__ f32x16 mfma_pieces(const u32x4 (&a)[NA], const u32x4 (&b)[NB], f32x16 acc)
+{
+    constexpr int kMost = NA > 2 || NB > 2 ? 2 : NA + NB;
+#pragma unroll
+    for (int i = NA - 1; i >= 0; --i)
+#pragma unroll
+        for (int j = NB - 1; j >= 0; --j)
+            if (i + j <= kMost) acc = mfma_bf16(a[i], b[j], acc);
+    return acc;
+}
+
+// Tiles in LDS: [piece][row][columns + 8]: rows 16 bytes apart from a multiple of the banks' width, so eight lanes that read 16 bytes of eight
+// rows meet in no bank.
+template <int DT>
+constexpr int kAttnPitch = 32 * DT + 8;
+
+template <int NQ, int DT, int ROWS>
+struct AttnTile {
+    uint16_t e[NQ][ROWS][kAttnPitch<DT>];
+};
+
+// A (or B) operand: row `row`, 8 columns from `col`.
+template <int NQ, int DT, int ROWS>
+__device__ __forceinline__ void read_rows(const AttnTile<NQ, DT, ROWS> &t, int row, int col, u32x4 (&out)[NQ])
+{
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) out[n] = *reinterpret_cast<const u32x4 *>(&t.e[n][row][col]);
+}
+
+__device__ __forceinline__ s16x4 read_transposed4(const uint16_t *p)
+{
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p));
+}
+
+// A operand of the transposed tile: its 32 columns from `col` as rows, its 16 rows from `row` as k, in the order of a result's registers.
+template <int NQ, int DT, int ROWS>
+__device__ __forceinline__ void read_columns(const AttnTile<NQ, DT, ROWS> &t, int row, int col, int lane, u32x4 (&out)[NQ])
+{
+    const int r = row + 4 * (lane >> 5) + ((lane & 15) >> 2), c = col + (lane & 16) + 4 * (lane & 3);
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const s16x4 lo = read_transposed4(&t.e[n][r][c]), hi = read_transposed4(&t.e[n][r + 8][c]);
+        s16x8 both;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) both[i] = lo[i], both[4 + i] = hi[i];
+        out[n] = __builtin_bit_cast(u32x4, both);
+    }
+}
+
+// Tokens [first, first + ROWS) of one head (of which those before `end` exist) into a tile.
+template <int NQ, int DT, int ROWS, bool CODES>
+__device__ __forceinline__ void load_tokens(AttnTile<NQ, DT, ROWS> &t, const void *x, int64_t base, int64_t stride, int first, int end, int dim,
+                                            const ElemFormat &f)
+{
+    constexpr int kEights = 4 * DT;
+#pragma unroll
+    for (int i = 0; i < ROWS * kEights / 256; ++i) {
+        const int n = threadIdx.x + 256 * i, row = n / kEights, col = (n % kEights) * 8;
+        const int count = first + row < end ? min(dim - col, 8) : 0;
+        float v[8];
+        if (count > 0) {
+            load8<CODES>(x, base + (first + row) * stride + col, count, v, f);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        }
+        u32x4 p[NQ];
+        bf16_pieces<NQ>(v, p);
+#pragma unroll
+        for (int k = 0; k < NQ; ++k) *reinterpret_cast<u32x4 *>(&t.e[k][row][col]) = p[k];
+    }
+}
+
+// 2^x; the vector unit's exponential flushes results below 2^-126, which is below 2^-24 of any sum that holds a 1.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Four results of a lane, columns col to col + 3 of which those below dim exist.  RESULT at run time: uniform.
+__device__ __forceinline__ void store4(void *y, int64_t at, int col, int dim, const float (&v)[4], int result, const ElemFormat &f)
+{
+    const int count = dim - col;
+    if (count <= 0) return;
+    float r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = v[i];
+    if (result != FMT_RESULT_F32) round_values(r, f);
+    if (result == FMT_RESULT_CODE16) {
+        uint16_t c[4];
+        encode_values(r, c, f);
+        uint16_t *d = static_cast<uint16_t *>(y) + at;
+        if (count >= 4) {
+            typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+            *reinterpret_cast<u16x4_any *>(d) = u16x4_any{c[0], c[1], c[2], c[3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < count) d[i] = c[i];
+        }
+    } else {
+        float *d = static_cast<float *>(y) + at;
+        if (count >= 4) {
+            *reinterpret_cast<f32x4_any *>(d) = f32x4_any{r[0], r[1], r[2], r[3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < count) d[i] = r[i];
+        }
+    }
+}
+
+// run(NQ, NP, DT, CODES) for a head size, the tensors' types and the format's stored mantissa bits.
+template <class RUN>
+void with_attention(int dim, int32_t store, int32_t result, int m, RUN &&run)
+{
+    using std::integral_constant;
+    auto pieces = [&](auto dt, auto codes) {
+        const bool whole = result == FMT_RESULT_F32;
+        if (m <= 7) {
+            if (whole) run(integral_constant<int, 1>{}, integral_constant<int, 3>{}, dt, codes);
+            else run(integral_constant<int, 1>{}, integral_constant<int, 1>{}, dt, codes);
+        } else {
+            if (whole) run(integral_constant<int, 2>{}, integral_constant<int, 3>{}, dt, codes);
+            else run(integral_constant<int, 2>{}, integral_constant<int, 2>{}, dt, codes);
+        }
+    };
+    auto sizes = [&](auto codes) {
+        if (dim <= 64) pieces(integral_constant<int, 2>{}, codes);
+        else pieces(integral_constant<int, 4>{}, codes);
+    };
+    if (store == FMT_STORE_CODE16) sizes(std::true_type{});
+    else sizes(std::false_type{});
+}
+
+}  // namespace fmt

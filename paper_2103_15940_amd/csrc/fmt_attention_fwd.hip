@@ -1,0 +1,216 @@
+// Attention, forward (fmt_attention.h has the mathematics and the layouts).
+#include <type_traits>
+
+#include "fmt_attention.h"
+
+namespace fmt {
+
+namespace {
+
+struct AttnFwd {
+    AttnShape s;
+    AttnView q, k, v, o;
+    float *lse;               // [batch][heads][q_len]
+    int32_t result;
+    int32_t splits;           // parts of a row's keys
+    float *part;              // splits > 1: [splits][batch * heads * q_len][dim] normalised outputs, then as many lse in base 2
+    ElemFormat f;
+};
+
+constexpr int kFwdRows = 128, kFwdKeys = 64;
+
+// A workgroup takes 128 rows of one (batch, kv head), a wave 32 of them: S^T = K Q^T gives every lane one row's scores, half of them each for
+// lanes l and l + 32, so the running maximum and sum of a row need one exchange per tile of 64 keys.
+template <int NQ, int NP, int DT, bool CODES>
+__global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
+{
+    __shared__ AttnTile<NQ, DT, kFwdKeys> ks, vs;
+    const AttnShape &s = a.s;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int b = blockIdx.z / a.splits, split = blockIdx.z % a.splits, kh = blockIdx.y;
+    const AttnSeq seq = attn_seq(s, b);
+    const int rows = s.q_len * s.group;
+    const int row0 = blockIdx.x * kFwdRows, row = row0 + wave * 32 + (lane & 31);
+    const int t = row / s.group, head = kh * s.group + row % s.group;
+    const bool live = row < rows;
+    const int pos = seq.first + t;
+    const int64_t i0 = static_cast<int64_t>(seq.first) + row0 / s.group;
+    const int64_t i1 = static_cast<int64_t>(seq.first) + (min(row0 + kFwdRows, rows) - 1) / s.group;
+
+    u32x4 q[2 * DT][NQ];
+#pragma unroll
+    for (int kk = 0; kk < 2 * DT; ++kk) {
+        const int col = 16 * kk + 8 * half, count = live ? min(s.dim - col, 8) : 0;
+        float v[8];
+        if (count > 0) {
+            load8<CODES>(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, count, v, a.f);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        }
+        bf16_pieces<NQ>(v, q[kk]);
+    }
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float top = -INFINITY, sum = 0.0f;
+    const int64_t kbase = b * a.k.sb + kh * a.k.sh, vbase = b * a.v.sb + kh * a.v.sh;
+    const AttnTiles tiles = attn_tiles(s, seq.length, i0, i1, kFwdKeys);
+    const int count = tiles.count();
+    const int begin = static_cast<int>(static_cast<int64_t>(count) * split / a.splits);
+    const int end = static_cast<int>(static_cast<int64_t>(count) * (split + 1) / a.splits);
+    for (int n = begin; n < end; ++n) {
+        const int k0 = tiles.at(n) * kFwdKeys;
+        __syncthreads();
+        load_tokens<NQ, DT, kFwdKeys, CODES>(ks, a.k.p, kbase, a.k.st, k0, seq.length, s.dim, a.f);
+        load_tokens<NQ, DT, kFwdKeys, CODES>(vs, a.v.p, vbase, a.v.st, k0, seq.length, s.dim, a.f);
+        __syncthreads();
+        f32x16 x[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[kt][i] = 0.0f;
+#pragma unroll
+            for (int kk = 0; kk < 2 * DT; ++kk) {
+                u32x4 f[NQ];
+                read_rows(ks, 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
+                x[kt] = mfma_pieces<NQ, NQ>(f, q[kk], x[kt]);
+            }
+        }
+        const bool all = attn_sees_all(s, seq.length, i0, i1, k0, k0 + kFwdKeys);
+        float high = top;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float y = x[kt][i] * s.scale2;
+                if (!all && !attn_sees(s, seq.length, pos, k0 + 32 * kt + 8 * (i / 4) + 4 * half + (i & 3))) y = -INFINITY;
+                x[kt][i] = y;
+                high = fmaxf(high, y);
+            }
+        high = fmaxf(high, __shfl_xor(high, 32));
+        const float base = high == -INFINITY ? 0.0f : high, shrink = exp2_fast(top - base);
+        top = high;
+        sum *= shrink;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] *= shrink;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                float p[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    p[j] = exp2_fast(x[kt][8 * kb + j] - base);
+                    sum += p[j];
+                }
+                u32x4 pp[NP];
+                bf16_pieces<NP>(p, pp);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    u32x4 f[NQ];
+                    read_columns(vs, 32 * kt + 16 * kb, 32 * d, lane, f);
+                    o[d] = mfma_pieces<NQ, NP>(f, pp, o[d]);
+                }
+            }
+    }
+    sum += __shfl_xor(sum, 32);
+    const float over = sum == 0.0f ? 0.0f : 1.0f / sum;          // a row that sees nothing: 0
+    if (!live) return;
+    const int64_t at = (static_cast<int64_t>(b) * s.heads + head) * s.q_len + t;
+    const float lse2 = sum == 0.0f ? -INFINITY : top + log2f(sum);
+    if (a.splits > 1) {
+        const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len;
+        float *out = a.part + (split * all_rows + at) * s.dim;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int col = 32 * d + 8 * g + 4 * half;
+                const float v[4] = {o[d][4 * g] * over, o[d][4 * g + 1] * over, o[d][4 * g + 2] * over, o[d][4 * g + 3] * over};
+                store4(out, col, col, s.dim, v, FMT_RESULT_F32, a.f);
+            }
+        if (half == 0) a.part[a.splits * all_rows * s.dim + split * all_rows + at] = lse2;
+        return;
+    }
+    const int64_t base = b * a.o.sb + t * a.o.st + head * a.o.sh;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int col = 32 * d + 8 * g + 4 * half;
+            const float v[4] = {o[d][4 * g] * over, o[d][4 * g + 1] * over, o[d][4 * g + 2] * over, o[d][4 * g + 3] * over};
+            store4(const_cast<void *>(a.o.p), base + col, col, s.dim, v, a.result, a.f);
+        }
+    if (half == 0 && a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
+}
+
+// Joins the parts of a row: one wave per row.
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnFwd a)
+{
+    const AttnShape &s = a.s;
+    const int lane = threadIdx.x & 63;
+    const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (at >= all_rows) return;
+    const float *lse = a.part + a.splits * all_rows * s.dim + at;
+    float top = -INFINITY;
+    for (int n = lane; n < a.splits; n += 64) top = fmaxf(top, lse[n * all_rows]);
+#pragma unroll
+    for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
+    const float base = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, o[2] = {0.0f, 0.0f};
+    for (int n = 0; n < a.splits; ++n) {
+        const float w = exp2_fast(lse[n * all_rows] - base);
+        sum += w;
+        const float *part = a.part + (n * all_rows + at) * s.dim;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (2 * lane + j < s.dim) o[j] = fmaf(w, part[2 * lane + j], o[j]);
+    }
+    const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int t = static_cast<int>(at % s.q_len), head = static_cast<int>(at / s.q_len % s.heads), b = static_cast<int>(at / s.q_len / s.heads);
+    float v[4] = {o[0] * over, o[1] * over, 0.0f, 0.0f};
+    if (2 * lane < s.dim)
+        store4(const_cast<void *>(a.o.p), b * a.o.sb + t * a.o.st + head * a.o.sh + 2 * lane, max(2 * lane, 0), min(s.dim, 2 * lane + 2), v, a.result,
+               a.f);
+    if (lane == 0 && a.lse) a.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
+}  // namespace
+
+int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &k, const AttnView &v, const AttnView &o, float *lse,
+                         int32_t store, int32_t result, const ElemFormat &f, int m, hipStream_t stream)
+{
+    int cus = 0;
+    int rc = device_cu_count(&cus);
+    if (rc != FMT_OK) return rc;
+    const int64_t row_tiles = (static_cast<int64_t>(s.q_len) * s.group + kFwdRows - 1) / kFwdRows;
+    // few rows, long keys: their keys in parts of four tiles or more, until the compute units have a workgroup each
+    const int64_t work = row_tiles * s.kv_heads * s.batch, key_tiles = (s.k_len + kFwdKeys - 1) / kFwdKeys;
+    int64_t splits = work >= cus ? 1 : (cus + work - 1) / work;
+    if (splits > key_tiles / 4) splits = key_tiles / 4;
+    if (splits < 1) splits = 1;
+    AttnFwd a{s, q, k, v, o, lse, result, static_cast<int32_t>(splits), nullptr, f};
+    const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len;
+    if (splits > 1) {
+        rc = get_acc_scratch(stream, static_cast<size_t>(splits * all_rows * (s.dim + 1)) * sizeof(float), &a.part);
+        if (rc != FMT_OK) return rc;
+    }
+    const dim3 grid(static_cast<uint32_t>(row_tiles), static_cast<uint32_t>(s.kv_heads), static_cast<uint32_t>(s.batch * splits));
+    auto go = [&](auto nq, auto np, auto dt, auto codes) {
+        attn_fwd_kernel<decltype(nq)::value, decltype(np)::value, decltype(dt)::value, decltype(codes)::value>
+            <<<grid, dim3(256), 0, stream>>>(a);
+    };
+    with_attention(s.dim, store, result, m, go);
+    if (splits > 1) attn_join_kernel<<<dim3(static_cast<uint32_t>((all_rows + 3) / 4)), dim3(256), 0, stream>>>(a);
+    FMT_HIP_CHECK(hipGetLastError());
+    return FMT_OK;
+}
+
+}  // namespace fmt

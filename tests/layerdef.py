@@ -78,7 +78,8 @@ def visible(q_len, k_len, length, first, causal, window, sinks):
 
 
 def attention(q, k, v, seen, scale, do=None):
-    """One head: q [m, d], k and v [n, d], seen [m, n].  (o, lse), and with do (o, lse, dq, dk, dv)."""
+    """One head: q [m, d], k and v [n, d], seen [m, n].  (o, lse), and with do (o, lse, dq, dk, dv).  P is an fp32 number: what lies
+    below its smallest normal one is 0."""
     q, k, v = (np.asarray(t, dtype=np.float64) for t in (q, k, v))
     used = seen.any(0)
     k, v = np.where(used[:, None], k, 0.0), np.where(used[:, None], v, 0.0)
@@ -89,6 +90,7 @@ def attention(q, k, v, seen, scale, do=None):
         total = p.sum(1, keepdims=True)
         lse = (np.where(np.isfinite(top), top, -np.inf) + np.log(total))[:, 0]
     p = p / np.where(total == 0, 1.0, total)
+    p = np.where(p < 2.0 ** -126, 0.0, p)
     o = p @ v
     if do is None:
         return o, lse

@@ -930,7 +930,7 @@ int fmt_attention_fwd(fmt_attention_t a, fmt_view_t q, fmt_view_t k, fmt_view_t 
                                    {{lse, 4 * (size_t)a.batch * (size_t)a.heads * (size_t)a.q_len, true}}, store, result, f, &e, &s);
     if (rc != FMT_OK) return rc;
     if (a.batch == 0 || a.heads == 0 || a.q_len == 0) return FMT_OK;
-    return launch_attention_fwd(s, attn_view(q), attn_view(k), attn_view(v), attn_view(o), lse, store, result, e, f.m,
+    return launch_attention_fwd(s, attn_view(q), attn_view(k), attn_view(v), attn_view(o), lse, store, result, e, f,
                                 static_cast<hipStream_t>(stream));
 }
 
@@ -949,7 +949,7 @@ int fmt_attention_bwd(fmt_attention_t a, fmt_view_t q, fmt_view_t k, fmt_view_t 
     if (a.batch == 0 || (a.heads == 0 && a.k_len == 0) || (a.q_len == 0 && a.k_len == 0)) return FMT_OK;
     if (!lse && a.heads > 0 && a.q_len > 0) return FMT_ERR_NULL;
     return launch_attention_bwd(s, attn_view(q), attn_view(k), attn_view(v), attn_view(o), attn_view(d_o), lse, attn_view(dq), attn_view(dk),
-                                attn_view(dv), store, result, e, f.m, static_cast<hipStream_t>(stream));
+                                attn_view(dv), store, result, e, f, static_cast<hipStream_t>(stream));
 }
 
 int fmt_format_info(fmt_format_t f, double *maxN, double *minN, double *minD,

@@ -193,6 +193,135 @@ __device__ __forceinline__ void load_tokens(AttnTile<NQ, DT, ROWS> &t, const voi
     }
 }
 
+// ---- operands as one fp16 value each
+//
+// Formats of at most 10 stored mantissa bits fit fp16's significand, and 1/5/10 and narrower its range as well: their products are exact in
+// one product instead of four of bf16 pieces.  For wider ranges (1/6/9, 1/8/7) values are taken times 2^9, which holds |x| < 2^7 and
+// their bits down to 2^-33; what a smaller element loses is below 2^-34, for a score less than 128 * 128 * 128 * 2^-33 = 2^-12 at the very worst (all
+// elements of one side at 2^7, all of the other below 2^-23) and below 2^-24 for elements up to 8.  A workgroup that meets an element of 2^7 or more, an infinity or
+// NaN, or whose V or dO lie below 2^-10 altogether, says so in a flag, and a second launch computes the results of flagged workgroups with pieces
+// of bf16; the others end at once (2 us for all).
+constexpr float kHalfUp = 512.0f, kHalfLimit = 128.0f, kHalfLeast = 0x1p-10f;
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ f32x16 mfma_f16(u32x4 a, u32x4 b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Eight fp32 values as N fp16 pieces, to nearest: 11 or 22 bits, and nothing below 2^-25.
+template <int N>
+__device__ __forceinline__ void f16_pieces(const float (&v)[8], u32x4 (&out)[N])
+{
+    f16x8 hi;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) hi[i] = static_cast<_Float16>(v[i]);
+    out[0] = __builtin_bit_cast(u32x4, hi);
+    if constexpr (N == 2) {
+        f16x8 lo;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lo[i] = static_cast<_Float16>(__fsub_rn(v[i], static_cast<float>(hi[i])));
+        out[1] = __builtin_bit_cast(u32x4, lo);
+    }
+}
+
+typedef uint32_t u32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// Eight elements as they lie in memory.
+template <bool CODES>
+struct RawEight {
+    u32x4 w[CODES ? 1 : 2];
+};
+
+template <bool CODES>
+__device__ __forceinline__ RawEight<CODES> raw_load(const void *x, int64_t at, int count)
+{
+    RawEight<CODES> r;
+    typedef std::conditional_t<CODES, u32x4_any2, u32x4_any4> u32x4_any;
+#pragma unroll
+    for (int n = 0; n < (CODES ? 1 : 2); ++n) r.w[n] = u32x4{0u, 0u, 0u, 0u};
+    if (count >= 8) {
+        const u32x4_any *s = reinterpret_cast<const u32x4_any *>(static_cast<const char *>(x) + at * (CODES ? 2 : 4));
+#pragma unroll
+        for (int n = 0; n < (CODES ? 1 : 2); ++n) r.w[n] = s[n];
+    } else if (count > 0) {
+        if constexpr (CODES) {
+            const uint16_t *s = static_cast<const uint16_t *>(x) + at;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) r.w[0][i / 2] |= static_cast<uint32_t>(s[i]) << (16 * (i & 1));
+        } else {
+            const uint32_t *s = static_cast<const uint32_t *>(x) + at;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) r.w[i / 4][i % 4] = s[i];
+        }
+    }
+    return r;
+}
+
+// Their values in fp32, rounded to the format.
+template <bool CODES>
+__device__ __forceinline__ void raw_values(const RawEight<CODES> &r, float (&v)[8], const ElemFormat &f)
+{
+    if constexpr (CODES) {
+        uint16_t c[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i] = static_cast<uint16_t>(r.w[0][i / 2] >> (16 * (i & 1)));
+        decode_values(c, v, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i / 4][i % 4]);
+        round_values(v, f);
+    }
+}
+
+// As fp16 times `up` (1: the format's values are fp16's; nothing is checked).  high: the largest |x| so far as a bit pattern (NaN above all).
+template <bool CODES>
+__device__ __forceinline__ u32x4 raw_half(const RawEight<CODES> &r, float up, uint32_t &high, const ElemFormat &f)
+{
+    if (CODES && f.codec == kCodecHalf) return r.w[0];
+    float v[8];
+    raw_values(r, v, f);
+    f16x8 h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        high = max(high, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+        h[i] = static_cast<_Float16>(v[i] * up);
+    }
+    return __builtin_bit_cast(u32x4, h);
+}
+
+// R(Q) is multiplied by the scale's sign, so that scores are ordered as they come out of the product; a scale of 0 makes it 0.
+__device__ __forceinline__ u32x4 half_signed(u32x4 q, float scale)
+{
+    const uint32_t flip = scale < 0.0f ? 0x80008000u : 0u, keep = scale == 0.0f ? 0u : 0xFFFFFFFFu;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i] = (q[i] ^ flip) & keep;
+    return q;
+}
+
+// P is taken times 2^14, so that its fp16 pieces hold their bits down to P = 2^-28.
+constexpr float kProbUp = 14.0f;
+
+// Whether a workgroup has to be computed with bf16 pieces: in all of its threads.  Every thread calls it.
+__device__ __forceinline__ bool half_flag(uint32_t high, uint32_t high_value)
+{
+    const bool over = __syncthreads_or(max(high, high_value) >= __float_as_uint(kHalfLimit));
+    const bool some = __syncthreads_or(high_value != 0u), large = __syncthreads_or(high_value >= __float_as_uint(kHalfLeast));
+    return over || (some && !large);
+}
+
+// Workgroups of one launch in an order that gives each of the 8 XCDs (workgroup i runs on XCD i % 8) a run of neighbours, which share keys
+// and values in its L2.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t i, uint32_t n)
+{
+    const uint32_t xcd = i & 7, each = n >> 3, more = n & 7;
+    return xcd * each + min(xcd, more) + (i >> 3);
+}
+
 // 2^x; the vector unit's exponential flushes results below 2^-126, which is below 2^-24 of any sum that holds a 1.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -243,6 +372,26 @@ void with_attention(int dim, int32_t store, int32_t result, int m, RUN &&run)
             if (whole) run(integral_constant<int, 2>{}, integral_constant<int, 3>{}, dt, codes);
             else run(integral_constant<int, 2>{}, integral_constant<int, 2>{}, dt, codes);
         }
+    };
+    auto sizes = [&](auto codes) {
+        if (dim <= 64) pieces(integral_constant<int, 2>{}, codes);
+        else pieces(integral_constant<int, 4>{}, codes);
+    };
+    if (store == FMT_STORE_CODE16) sizes(std::true_type{});
+    else sizes(std::false_type{});
+}
+
+// Whether a format's values go as one fp16 value each.
+inline bool attention_half(fmt_format_t f) { return f.m <= 10; }
+
+// run(NP, DT, CODES) for the fp16 operands: one piece of P (11 bits) where results have 8, two (22) where they have more.
+template <class RUN>
+void with_attention_half(int dim, int32_t store, int32_t result, fmt_format_t f, RUN &&run)
+{
+    using std::integral_constant;
+    auto pieces = [&](auto dt, auto codes) {
+        if (result == FMT_RESULT_F32 || f.m > 7) run(integral_constant<int, 2>{}, dt, codes);
+        else run(integral_constant<int, 1>{}, dt, codes);
     };
     auto sizes = [&](auto codes) {
         if (dim <= 64) pieces(integral_constant<int, 2>{}, codes);

@@ -280,7 +280,7 @@ __global__ __launch_bounds__(256) void attn_dkv_kernel(AttnBwd a)
 
 int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &k, const AttnView &v, const AttnView &o, const AttnView &go,
                          const float *lse, const AttnView &dq, const AttnView &dk, const AttnView &dv, int32_t store, int32_t result,
-                         const ElemFormat &f, int m, hipStream_t stream)
+                         const ElemFormat &f, fmt_format_t fmt, hipStream_t stream)
 {
     AttnBwd a{s, q, k, v, o, go, dq, dk, dv, lse, nullptr, result, f};
     const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len;
@@ -294,7 +294,7 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
     const uint32_t row_tiles = static_cast<uint32_t>((static_cast<int64_t>(a.s.q_len) * s.group + kRowTile - 1) / kRowTile);
     const uint32_t key_tiles = static_cast<uint32_t>((s.k_len + kKvKeys - 1) / kKvKeys);
     const uint32_t kv_heads = static_cast<uint32_t>(s.kv_heads), batch = static_cast<uint32_t>(s.batch);
-    with_attention(s.dim, store, result, m, [&](auto nq, auto np, auto dt, auto codes) {
+    with_attention(s.dim, store, result, fmt.m, [&](auto nq, auto np, auto dt, auto codes) {
         constexpr int NQ = decltype(nq)::value, NP = decltype(np)::value, DT = decltype(dt)::value;
         constexpr bool CODES = decltype(codes)::value;
         auto go2 = [&](auto g) {

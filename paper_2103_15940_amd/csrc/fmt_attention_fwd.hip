@@ -14,10 +14,52 @@ struct AttnFwd {
     int32_t result;
     int32_t splits;           // parts of a row's keys
     float *part;              // splits > 1: [splits][batch * heads * q_len][dim] normalised outputs, then as many lse in base 2
+    uint32_t *flags;          // per workgroup: whether it is left to the pieces of bf16; or nullptr
+    float up;                 // what the fp16 operands are multiplied by
+    int32_t row_tiles;
     ElemFormat f;
 };
 
 constexpr int kFwdRows = 128, kFwdKeys = 64;
+
+struct FwdBlock {
+    uint32_t id;
+    int b, kh, split, row0;
+};
+
+// Which rows a workgroup takes.  The later ones of a causal mask see more keys: they go first.
+__device__ __forceinline__ FwdBlock fwd_block(const AttnFwd &a)
+{
+    const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
+    const uint32_t tile = id % a.row_tiles, rest = id / a.row_tiles;
+    const uint32_t kh = rest % a.s.kv_heads, rest2 = rest / a.s.kv_heads;
+    return FwdBlock{id, static_cast<int>(rest2 / a.splits), static_cast<int>(kh), static_cast<int>(rest2 % a.splits),
+                    static_cast<int>(a.s.causal ? a.row_tiles - 1 - tile : tile) * kFwdRows};
+}
+
+// A lane's outputs: its row of a wave's results, over its sum.
+template <int DT>
+__device__ __forceinline__ void fwd_store(const AttnFwd &a, const f32x16 (&o)[DT], int split, int b, int t, int head, int half, float over, float lse2)
+{
+    const AttnShape &s = a.s;
+    const int64_t at = (static_cast<int64_t>(b) * s.heads + head) * s.q_len + t;
+    const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len;
+    const bool part = a.splits > 1;
+    void *out = part ? static_cast<void *>(a.part) : const_cast<void *>(a.o.p);
+    const int64_t base = part ? (split * all_rows + at) * s.dim : b * a.o.sb + t * a.o.st + head * a.o.sh;
+    const int result = part ? FMT_RESULT_F32 : a.result;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int col = 32 * d + 8 * g + 4 * half;
+            const float v[4] = {o[d][4 * g] * over, o[d][4 * g + 1] * over, o[d][4 * g + 2] * over, o[d][4 * g + 3] * over};
+            store4(out, base + col, col, s.dim, v, result, a.f);
+        }
+    if (half != 0) return;
+    if (part) a.part[a.splits * all_rows * s.dim + split * all_rows + at] = lse2;
+    else if (a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
+}
 
 // A workgroup takes 128 rows of one (batch, kv head), a wave 32 of them: S^T = K Q^T gives every lane one row's scores, half of them each for
 // lanes l and l + 32, so the running maximum and sum of a row need one exchange per tile of 64 keys.
@@ -27,10 +69,12 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
     __shared__ AttnTile<NQ, DT, kFwdKeys> ks, vs;
     const AttnShape &s = a.s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-    const int b = blockIdx.z / a.splits, split = blockIdx.z % a.splits, kh = blockIdx.y;
+    const FwdBlock blk = fwd_block(a);
+    if (a.flags && a.flags[blk.id] == 0) return;
+    const int b = blk.b, split = blk.split, kh = blk.kh;
     const AttnSeq seq = attn_seq(s, b);
     const int rows = s.q_len * s.group;
-    const int row0 = blockIdx.x * kFwdRows, row = row0 + wave * 32 + (lane & 31);
+    const int row0 = blk.row0, row = row0 + wave * 32 + (lane & 31);
     const int t = row / s.group, head = kh * s.group + row % s.group;
     const bool live = row < rows;
     const int pos = seq.first + t;
@@ -121,33 +165,137 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
     }
     sum += __shfl_xor(sum, 32);
     const float over = sum == 0.0f ? 0.0f : 1.0f / sum;          // a row that sees nothing: 0
-    if (!live) return;
-    const int64_t at = (static_cast<int64_t>(b) * s.heads + head) * s.q_len + t;
-    const float lse2 = sum == 0.0f ? -INFINITY : top + log2f(sum);
-    if (a.splits > 1) {
-        const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len;
-        float *out = a.part + (split * all_rows + at) * s.dim;
+    if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, sum == 0.0f ? -INFINITY : top + log2f(sum));
+}
+
+// The same on operands of one fp16 value each, P in NP pieces of fp16.  The next tile's elements are on their way from memory while a
+// tile is computed; they are rounded and converted on their way into the other of two LDS buffers, so a tile costs one barrier.
+template <int NP, int DT, bool CODES>
+__global__ __launch_bounds__(256, 2) void attn_fwd_half_kernel(AttnFwd a)
+{
+    __shared__ AttnTile<1, DT, kFwdKeys> ks[2], vs[2];
+    constexpr int kEights = 4 * DT, kLoads = kFwdKeys * kEights / 256;
+    const AttnShape &s = a.s;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const FwdBlock blk = fwd_block(a);
+    const int b = blk.b, split = blk.split, kh = blk.kh;
+    const AttnSeq seq = attn_seq(s, b);
+    const int rows = s.q_len * s.group;
+    const int row0 = blk.row0, row = row0 + wave * 32 + (lane & 31);
+    const int t = row / s.group, head = kh * s.group + row % s.group;
+    const bool live = row < rows;
+    const int pos = seq.first + t;
+    const int64_t i0 = static_cast<int64_t>(seq.first) + row0 / s.group;
+    const int64_t i1 = static_cast<int64_t>(seq.first) + (min(row0 + kFwdRows, rows) - 1) / s.group;
+    uint32_t high = 0, high_value = 0;
+
+    const int64_t kbase = b * a.k.sb + kh * a.k.sh, vbase = b * a.v.sb + kh * a.v.sh;
+    const AttnTiles tiles = attn_tiles(s, seq.length, i0, i1, kFwdKeys);
+    const int count = tiles.count();
+    const int begin = static_cast<int>(static_cast<int64_t>(count) * split / a.splits);
+    const int end = static_cast<int>(static_cast<int64_t>(count) * (split + 1) / a.splits);
+    RawEight<CODES> kr[kLoads], vr[kLoads];
+    const int key_in = threadIdx.x / kEights, col_in = (threadIdx.x % kEights) * 8;     // + 256 / kEights keys per load
+    auto fetch = [&](int n) __attribute__((always_inline)) {
+        const int k0 = tiles.at(n) * kFwdKeys;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int i = 0; i < kLoads; ++i) {
+            const int key = k0 + key_in + i * (256 / kEights);
+            const int have = key < seq.length ? s.dim - col_in : 0;
+            kr[i] = raw_load<CODES>(a.k.p, kbase + key * a.k.st + col_in, have);
+            vr[i] = raw_load<CODES>(a.v.p, vbase + key * a.v.st + col_in, have);
+        }
+    };
+    if (begin < end) fetch(begin);
+
+    u32x4 q[2 * DT];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int col = 32 * d + 8 * g + 4 * half;
-                const float v[4] = {o[d][4 * g] * over, o[d][4 * g + 1] * over, o[d][4 * g + 2] * over, o[d][4 * g + 3] * over};
-                store4(out, col, col, s.dim, v, FMT_RESULT_F32, a.f);
-            }
-        if (half == 0) a.part[a.splits * all_rows * s.dim + split * all_rows + at] = lse2;
-        return;
+    for (int kk = 0; kk < 2 * DT; ++kk) {
+        const int col = 16 * kk + 8 * half;
+        q[kk] = half_signed(
+            raw_half<CODES>(raw_load<CODES>(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, live ? s.dim - col : 0), a.up, high, a.f), s.scale);
     }
-    const int64_t base = b * a.o.sb + t * a.o.st + head * a.o.sh;
+    f32x16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int col = 32 * d + 8 * g + 4 * half;
-            const float v[4] = {o[d][4 * g] * over, o[d][4 * g + 1] * over, o[d][4 * g + 2] * over, o[d][4 * g + 3] * over};
-            store4(const_cast<void *>(a.o.p), base + col, col, s.dim, v, a.result, a.f);
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float top = -INFINITY, sum = 0.0f;
+    const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up);
+    for (int n = begin; n < end; ++n) {
+        const int k0 = tiles.at(n) * kFwdKeys, buf = (n - begin) & 1;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int key = key_in + i * (256 / kEights);
+            *reinterpret_cast<u32x4 *>(&ks[buf].e[0][key][col_in]) = raw_half<CODES>(kr[i], a.up, high, a.f);
+            *reinterpret_cast<u32x4 *>(&vs[buf].e[0][key][col_in]) = raw_half<CODES>(vr[i], a.up, high_value, a.f);
         }
-    if (half == 0 && a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
+        __syncthreads();
+        if (n + 1 < end) fetch(n + 1);
+        f32x16 x[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[kt][i] = 0.0f;
+#pragma unroll
+            for (int kk = 0; kk < 2 * DT; ++kk) {
+                u32x4 f[1];
+                read_rows(ks[buf], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
+                x[kt] = mfma_f16(f[0], q[kk], x[kt]);
+            }
+        }
+        if (!attn_sees_all(s, seq.length, i0, i1, k0, k0 + kFwdKeys)) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!attn_sees(s, seq.length, pos, k0 + 32 * kt + 8 * (i / 4) + 4 * half + (i & 3))) x[kt][i] = -INFINITY;
+        }
+        float high_score = -INFINITY;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) high_score = fmaxf(high_score, x[kt][i]);
+        high_score = fmaxf(high_score, __shfl_xor(high_score, 32)) * scale2;
+        if (__any(high_score > top)) {                    // else the running maximum stays in all of the wave's rows
+            const float next = fmaxf(top, high_score);
+            const float shrink = next == -INFINITY ? 1.0f : exp2_fast(top - next);
+            top = next;
+            sum *= shrink;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= shrink;
+        }
+        const float base = (top == -INFINITY ? 0.0f : top) - kProbUp;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                float p[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    p[j] = exp2_fast(fmaf(x[kt][8 * kb + j], scale2, -base));
+                    sum += p[j];
+                }
+                u32x4 pp[NP];
+                f16_pieces<NP>(p, pp);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    u32x4 f[1];
+                    read_columns(vs[buf], 32 * kt + 16 * kb, 32 * d, lane, f);
+#pragma unroll
+                    for (int w = NP - 1; w >= 0; --w) o[d] = mfma_f16(f[0], pp[w], o[d]);
+                }
+            }
+    }
+    sum += __shfl_xor(sum, 32);
+    const float over = sum == 0.0f ? 0.0f : 1.0f / (sum * a.up);
+    if (a.flags) {
+        const bool flag = half_flag(high, high_value);
+        if (threadIdx.x == 0) a.flags[blk.id] = flag;
+    }
+    if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, sum == 0.0f ? -INFINITY : top - kProbUp + log2f(sum));
 }
 
 // Joins the parts of a row: one wave per row.
@@ -185,7 +333,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnFwd a)
 }  // namespace
 
 int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &k, const AttnView &v, const AttnView &o, float *lse,
-                         int32_t store, int32_t result, const ElemFormat &f, int m, hipStream_t stream)
+                         int32_t store, int32_t result, const ElemFormat &f, fmt_format_t fmt, hipStream_t stream)
 {
     int cus = 0;
     int rc = device_cu_count(&cus);
@@ -196,18 +344,30 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
     int64_t splits = work >= cus ? 1 : (cus + work - 1) / work;
     if (splits > key_tiles / 4) splits = key_tiles / 4;
     if (splits < 1) splits = 1;
-    AttnFwd a{s, q, k, v, o, lse, result, static_cast<int32_t>(splits), nullptr, f};
-    const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len;
-    if (splits > 1) {
-        rc = get_acc_scratch(stream, static_cast<size_t>(splits * all_rows * (s.dim + 1)) * sizeof(float), &a.part);
+    AttnFwd a{s, q, k, v, o, lse, result, static_cast<int32_t>(splits), nullptr, nullptr, 1.0f, static_cast<int32_t>(row_tiles), f};
+    const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len, grid = work * splits;
+    if (grid > 0x7FFFFFFF) return FMT_ERR_SHAPE;
+    const bool half = attention_half(fmt), flagged = half && fmt.e > 5;
+    const size_t part = splits > 1 ? static_cast<size_t>(splits * all_rows * (s.dim + 1)) : 0, flags = flagged ? static_cast<size_t>(grid) : 0;
+    if (part + flags) {
+        float *scratch = nullptr;
+        rc = get_acc_scratch(stream, (part + flags) * sizeof(float), &scratch);
         if (rc != FMT_OK) return rc;
+        if (part) a.part = scratch;
+        if (flagged) a.flags = reinterpret_cast<uint32_t *>(scratch + part);
     }
-    const dim3 grid(static_cast<uint32_t>(row_tiles), static_cast<uint32_t>(s.kv_heads), static_cast<uint32_t>(s.batch * splits));
-    auto go = [&](auto nq, auto np, auto dt, auto codes) {
-        attn_fwd_kernel<decltype(nq)::value, decltype(np)::value, decltype(dt)::value, decltype(codes)::value>
-            <<<grid, dim3(256), 0, stream>>>(a);
-    };
-    with_attention(s.dim, store, result, m, go);
+    const dim3 blocks(static_cast<uint32_t>(grid));
+    if (half) {
+        a.up = flagged ? kHalfUp : 1.0f;
+        with_attention_half(s.dim, store, result, fmt, [&](auto np, auto dt, auto codes) {
+            attn_fwd_half_kernel<decltype(np)::value, decltype(dt)::value, decltype(codes)::value><<<blocks, dim3(256), 0, stream>>>(a);
+        });
+    }
+    if (!half || flagged)
+        with_attention(s.dim, store, result, fmt.m, [&](auto nq, auto np, auto dt, auto codes) {
+            attn_fwd_kernel<decltype(nq)::value, decltype(np)::value, decltype(dt)::value, decltype(codes)::value>
+                <<<blocks, dim3(256), 0, stream>>>(a);
+        });
     if (splits > 1) attn_join_kernel<<<dim3(static_cast<uint32_t>((all_rows + 3) / 4)), dim3(256), 0, stream>>>(a);
     FMT_HIP_CHECK(hipGetLastError());
     return FMT_OK;

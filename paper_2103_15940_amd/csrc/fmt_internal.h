@@ -196,7 +196,7 @@ int launch_layernorm_bwd(const LayerNorm &n, const void *dy, int64_t lddy, const
                          const float *rstd, const float *gamma, void *dz, int64_t lddz, void *dx, int64_t lddx, float *dgamma,
                          float *dbeta, const ElemFormat &f, hipStream_t stream);
 
-// Attention (fmt_attention_fwd.hip, fmt_attention_bwd.hip); m: stored mantissa bits of the format.
+// Attention (fmt_attention_fwd.hip, fmt_attention_bwd.hip).
 struct AttnView {
     const void *p;
     int64_t sb, st, sh;       // strides of batch, token and head
@@ -211,10 +211,10 @@ struct AttnShape {
 
 constexpr int kAttnMaxDim = 128;
 int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &k, const AttnView &v, const AttnView &o, float *lse,
-                         int32_t store, int32_t result, const ElemFormat &f, int m, hipStream_t stream);
+                         int32_t store, int32_t result, const ElemFormat &f, fmt_format_t fmt, hipStream_t stream);
 int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &k, const AttnView &v, const AttnView &o, const AttnView &go,
                          const float *lse, const AttnView &dq, const AttnView &dk, const AttnView &dv, int32_t store, int32_t result,
-                         const ElemFormat &f, int m, hipStream_t stream);
+                         const ElemFormat &f, fmt_format_t fmt, hipStream_t stream);
 
 // Reports a failed HIP call on stderr when the environment variable FMT_VERBOSE is set.
 void report_hip_error(const char *expr, const char *file, int line, hipError_t err);

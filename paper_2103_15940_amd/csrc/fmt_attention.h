@@ -9,10 +9,9 @@
 // Heads that share keys and values are taken as rows of one product: row r is query r / group of head r % group of the group, so a
 // tile of keys is read once for all of them, and gradients of shared keys and values add up in the accumulators.
 //
-// Operands are split exactly into NQ bf16 pieces (1: 1/8/7 and narrower, 2: up to 16 significant bits), whose products are exact in
-// the matrix cores and added in fp32.  P and dS, which are fp32, go in NP pieces: 3 hold all of their 24 bits (results in
-// unrounded fp32), 1 or 2 hold as many as the operands have (results that are rounded to the format).  Products of pieces that lie
-// below 2^-24 of the largest are left out.
+// Operands go as one fp16 value each where their range allows, P and dS in one or two fp16 pieces (below).  Otherwise they go in two bf16
+// pieces (up to 16 significant bits, fp32's range), whose products are exact in the matrix cores and added in fp32, and P and dS in
+// three, which hold all of their 24 bits; products of pieces that lie below 2^-24 of the largest are left out.
 //
 // Layout of v_mfma_f32_32x32x16: A gives lane l row l % 32 and the 8 k from 8 (l / 32); B the same with columns; the result gives lane l column
 // l % 32, and its register i row 8 (i / 4) + 4 (l / 32) + i % 4.  So registers 8b to 8b + 7 of a result are, as they stand, a B operand for
@@ -170,18 +169,18 @@ __device__ __forceinline__ void read_columns(const AttnTile<NQ, DT, ROWS> &t, in
 }
 
 // Tokens [first, first + ROWS) of one head (of which those before `end` exist) into a tile.
-template <int NQ, int DT, int ROWS, bool CODES>
+template <int NQ, int DT, int ROWS>
 __device__ __forceinline__ void load_tokens(AttnTile<NQ, DT, ROWS> &t, const void *x, int64_t base, int64_t stride, int first, int end, int dim,
-                                            const ElemFormat &f)
+                                            bool codes, const ElemFormat &f)
 {
     constexpr int kEights = 4 * DT;
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < ROWS * kEights / 256; ++i) {
         const int n = threadIdx.x + 256 * i, row = n / kEights, col = (n % kEights) * 8;
         const int count = first + row < end ? min(dim - col, 8) : 0;
         float v[8];
         if (count > 0) {
-            load8<CODES>(x, base + (first + row) * stride + col, count, v, f);
+            load8_any(x, base + (first + row) * stride + col, count, v, codes, f);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = 0.0f;
@@ -278,13 +277,9 @@ __device__ __forceinline__ void raw_values(const RawEight<CODES> &r, float (&v)[
     }
 }
 
-// As fp16 times `up` (1: the format's values are fp16's; nothing is checked).  high: the largest |x| so far as a bit pattern (NaN above all).
-template <bool CODES>
-__device__ __forceinline__ u32x4 raw_half(const RawEight<CODES> &r, float up, uint32_t &high, const ElemFormat &f)
+// fp32 values as fp16 times `up`.  high: the largest |x| so far as a bit pattern (NaN above all).
+__device__ __forceinline__ u32x4 to_half(const float (&v)[8], float up, uint32_t &high)
 {
-    if (CODES && f.codec == kCodecHalf) return r.w[0];
-    float v[8];
-    raw_values(r, v, f);
     f16x8 h;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -292,6 +287,16 @@ __device__ __forceinline__ u32x4 raw_half(const RawEight<CODES> &r, float up, ui
         h[i] = static_cast<_Float16>(v[i] * up);
     }
     return __builtin_bit_cast(u32x4, h);
+}
+
+// As fp16 times `up` (1: the format's values are fp16's; nothing is checked).
+template <bool CODES>
+__device__ __forceinline__ u32x4 raw_half(const RawEight<CODES> &r, float up, uint32_t &high, const ElemFormat &f)
+{
+    if (CODES && f.codec == kCodecHalf) return r.w[0];
+    float v[8];
+    raw_values(r, v, f);
+    return to_half(v, up, high);
 }
 
 // R(Q) is multiplied by the scale's sign, so that scores are ordered as they come out of the product; a scale of 0 makes it 0.
@@ -358,47 +363,20 @@ __device__ __forceinline__ void store4(void *y, int64_t at, int col, int dim, co
     }
 }
 
-// run(NQ, NP, DT, CODES) for a head size, the tensors' types and the format's stored mantissa bits.
+// run(DT) for a head size.
 template <class RUN>
-void with_attention(int dim, int32_t store, int32_t result, int m, RUN &&run)
+void with_dim(int dim, RUN &&run)
 {
-    using std::integral_constant;
-    auto pieces = [&](auto dt, auto codes) {
-        const bool whole = result == FMT_RESULT_F32;
-        if (m <= 7) {
-            if (whole) run(integral_constant<int, 1>{}, integral_constant<int, 3>{}, dt, codes);
-            else run(integral_constant<int, 1>{}, integral_constant<int, 1>{}, dt, codes);
-        } else {
-            if (whole) run(integral_constant<int, 2>{}, integral_constant<int, 3>{}, dt, codes);
-            else run(integral_constant<int, 2>{}, integral_constant<int, 2>{}, dt, codes);
-        }
-    };
-    auto sizes = [&](auto codes) {
-        if (dim <= 64) pieces(integral_constant<int, 2>{}, codes);
-        else pieces(integral_constant<int, 4>{}, codes);
-    };
-    if (store == FMT_STORE_CODE16) sizes(std::true_type{});
-    else sizes(std::false_type{});
+    if (dim <= 64) run(std::integral_constant<int, 2>{});
+    else run(std::integral_constant<int, 4>{});
 }
+
+constexpr int kPieces = 2, kProbPieces = 3;      // bf16 pieces of operands, of P and dS
 
 // Whether a format's values go as one fp16 value each.
 inline bool attention_half(fmt_format_t f) { return f.m <= 10; }
 
-// run(NP, DT, CODES) for the fp16 operands: one piece of P (11 bits) where results have 8, two (22) where they have more.
-template <class RUN>
-void with_attention_half(int dim, int32_t store, int32_t result, fmt_format_t f, RUN &&run)
-{
-    using std::integral_constant;
-    auto pieces = [&](auto dt, auto codes) {
-        if (result == FMT_RESULT_F32 || f.m > 7) run(integral_constant<int, 2>{}, dt, codes);
-        else run(integral_constant<int, 1>{}, dt, codes);
-    };
-    auto sizes = [&](auto codes) {
-        if (dim <= 64) pieces(integral_constant<int, 2>{}, codes);
-        else pieces(integral_constant<int, 4>{}, codes);
-    };
-    if (store == FMT_STORE_CODE16) sizes(std::true_type{});
-    else sizes(std::false_type{});
-}
+// Pieces of P and dS with fp16 operands: one (11 bits) where results have 8, two (22) where they have more.
+inline int half_pieces(fmt_format_t f, int32_t result) { return result == FMT_RESULT_F32 || f.m > 7 ? 2 : 1; }
 
 }  // namespace fmt

@@ -1,4 +1,5 @@
 // Attention, forward (fmt_attention.h has the mathematics and the layouts).
+#include <algorithm>
 #include <type_traits>
 
 #include "fmt_attention.h"
@@ -17,6 +18,8 @@ struct AttnFwd {
     uint32_t *flags;          // per workgroup: whether it is left to the pieces of bf16; or nullptr
     float up;                 // what the fp16 operands are multiplied by
     int32_t row_tiles;
+    uint32_t blocks;          // workgroups of the first launch
+    bool codes;               // how q, k and v are stored
     ElemFormat f;
 };
 
@@ -28,9 +31,8 @@ struct FwdBlock {
 };
 
 // Which rows a workgroup takes.  The later ones of a causal mask see more keys: they go first.
-__device__ __forceinline__ FwdBlock fwd_block(const AttnFwd &a)
+__device__ __forceinline__ FwdBlock fwd_block(const AttnFwd &a, uint32_t id)
 {
-    const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
     const uint32_t tile = id % a.row_tiles, rest = id / a.row_tiles;
     const uint32_t kh = rest % a.s.kv_heads, rest2 = rest / a.s.kv_heads;
     return FwdBlock{id, static_cast<int>(rest2 / a.splits), static_cast<int>(kh), static_cast<int>(rest2 % a.splits),
@@ -63,14 +65,13 @@ __device__ __forceinline__ void fwd_store(const AttnFwd &a, const f32x16 (&o)[DT
 
 // A workgroup takes 128 rows of one (batch, kv head), a wave 32 of them: S^T = K Q^T gives every lane one row's scores, half of them each for
 // lanes l and l + 32, so the running maximum and sum of a row need one exchange per tile of 64 keys.
-template <int NQ, int NP, int DT, bool CODES>
-__global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
+template <int DT>
+__device__ __forceinline__ void fwd_pieces(const AttnFwd &a, uint32_t id, AttnTile<kPieces, DT, kFwdKeys> &ks, AttnTile<kPieces, DT, kFwdKeys> &vs)
 {
-    __shared__ AttnTile<NQ, DT, kFwdKeys> ks, vs;
+    constexpr int NQ = kPieces, NP = kProbPieces;
     const AttnShape &s = a.s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-    const FwdBlock blk = fwd_block(a);
-    if (a.flags && a.flags[blk.id] == 0) return;
+    const FwdBlock blk = fwd_block(a, id);
     const int b = blk.b, split = blk.split, kh = blk.kh;
     const AttnSeq seq = attn_seq(s, b);
     const int rows = s.q_len * s.group;
@@ -87,7 +88,7 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
         const int col = 16 * kk + 8 * half, count = live ? min(s.dim - col, 8) : 0;
         float v[8];
         if (count > 0) {
-            load8<CODES>(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, count, v, a.f);
+            load8_any(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, count, v, a.codes, a.f);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = 0.0f;
@@ -109,8 +110,8 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
     for (int n = begin; n < end; ++n) {
         const int k0 = tiles.at(n) * kFwdKeys;
         __syncthreads();
-        load_tokens<NQ, DT, kFwdKeys, CODES>(ks, a.k.p, kbase, a.k.st, k0, seq.length, s.dim, a.f);
-        load_tokens<NQ, DT, kFwdKeys, CODES>(vs, a.v.p, vbase, a.v.st, k0, seq.length, s.dim, a.f);
+        load_tokens<NQ, DT, kFwdKeys>(ks, a.k.p, kbase, a.k.st, k0, seq.length, s.dim, a.codes, a.f);
+        load_tokens<NQ, DT, kFwdKeys>(vs, a.v.p, vbase, a.v.st, k0, seq.length, s.dim, a.codes, a.f);
         __syncthreads();
         f32x16 x[2];
 #pragma unroll
@@ -168,6 +169,17 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
     if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, sum == 0.0f ? -INFINITY : top + log2f(sum));
 }
 
+// All workgroups of a launch (no flags), or those that the launch before has flagged, among few that stay.
+template <int DT>
+__global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
+{
+    __shared__ AttnTile<kPieces, DT, kFwdKeys> ks, vs;
+    for (uint32_t i = blockIdx.x; i < a.blocks; i += gridDim.x) {
+        const uint32_t id = xcd_order(i, a.blocks);
+        if (a.flags == nullptr || a.flags[id] != 0) fwd_pieces<DT>(a, id, ks, vs);       // (the same in the whole workgroup)
+    }
+}
+
 // The same on operands of one fp16 value each, P in NP pieces of fp16.  The next tile's elements are on their way from memory while a
 // tile is computed; they are rounded and converted on their way into the other of two LDS buffers, so a tile costs one barrier.
 template <int NP, int DT, bool CODES>
@@ -177,7 +189,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_half_kernel(AttnFwd a)
     constexpr int kEights = 4 * DT, kLoads = kFwdKeys * kEights / 256;
     const AttnShape &s = a.s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
-    const FwdBlock blk = fwd_block(a);
+    const FwdBlock blk = fwd_block(a, xcd_order(blockIdx.x, gridDim.x));
     const int b = blk.b, split = blk.split, kh = blk.kh;
     const AttnSeq seq = attn_seq(s, b);
     const int rows = s.q_len * s.group;
@@ -344,7 +356,7 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
     int64_t splits = work >= cus ? 1 : (cus + work - 1) / work;
     if (splits > key_tiles / 4) splits = key_tiles / 4;
     if (splits < 1) splits = 1;
-    AttnFwd a{s, q, k, v, o, lse, result, static_cast<int32_t>(splits), nullptr, nullptr, 1.0f, static_cast<int32_t>(row_tiles), f};
+    AttnFwd a{s, q, k, v, o, lse, result, static_cast<int32_t>(splits), nullptr, nullptr, 1.0f, static_cast<int32_t>(row_tiles), 0, false, f};
     const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len, grid = work * splits;
     if (grid > 0x7FFFFFFF) return FMT_ERR_SHAPE;
     const bool half = attention_half(fmt), flagged = half && fmt.e > 5;
@@ -356,18 +368,22 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
         if (part) a.part = scratch;
         if (flagged) a.flags = reinterpret_cast<uint32_t *>(scratch + part);
     }
-    const dim3 blocks(static_cast<uint32_t>(grid));
-    if (half) {
-        a.up = flagged ? kHalfUp : 1.0f;
-        with_attention_half(s.dim, store, result, fmt, [&](auto np, auto dt, auto codes) {
-            attn_fwd_half_kernel<decltype(np)::value, decltype(dt)::value, decltype(codes)::value><<<blocks, dim3(256), 0, stream>>>(a);
-        });
-    }
-    if (!half || flagged)
-        with_attention(s.dim, store, result, fmt.m, [&](auto nq, auto np, auto dt, auto codes) {
-            attn_fwd_kernel<decltype(nq)::value, decltype(np)::value, decltype(dt)::value, decltype(codes)::value>
-                <<<blocks, dim3(256), 0, stream>>>(a);
-        });
+    a.blocks = static_cast<uint32_t>(grid);
+    a.codes = store == FMT_STORE_CODE16;
+    with_dim(s.dim, [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (half) {
+            a.up = flagged ? kHalfUp : 1.0f;
+            const dim3 blocks(a.blocks), threads(256);
+            const bool two = half_pieces(fmt, result) == 2;
+            if (two && a.codes) attn_fwd_half_kernel<2, DT, true><<<blocks, threads, 0, stream>>>(a);
+            else if (two) attn_fwd_half_kernel<2, DT, false><<<blocks, threads, 0, stream>>>(a);
+            else if (a.codes) attn_fwd_half_kernel<1, DT, true><<<blocks, threads, 0, stream>>>(a);
+            else attn_fwd_half_kernel<1, DT, false><<<blocks, threads, 0, stream>>>(a);
+        }
+        if (!half || flagged)
+            attn_fwd_kernel<DT><<<dim3(flagged ? std::min(a.blocks, static_cast<uint32_t>(cus)) : a.blocks), dim3(256), 0, stream>>>(a);
+    });
     if (splits > 1) attn_join_kernel<<<dim3(static_cast<uint32_t>((all_rows + 3) / 4)), dim3(256), 0, stream>>>(a);
     FMT_HIP_CHECK(hipGetLastError());
     return FMT_OK;

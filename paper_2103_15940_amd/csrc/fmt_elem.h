@@ -139,4 +139,11 @@ __device__ __forceinline__ void store8(void *y, int64_t at, int count, float (&v
     }
 }
 
+// The same with the type known at run time (uniform).
+__device__ __forceinline__ void load8_any(const void *x, int64_t at, int count, float (&v)[8], bool codes, const ElemFormat &f)
+{
+    if (codes) load8<true>(x, at, count, v, f);
+    else load8<false>(x, at, count, v, f);
+}
+
 }  // namespace fmt

@@ -27,6 +27,7 @@
 namespace fmt {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -50,6 +51,39 @@ __device__ __forceinline__ bool attn_sees(const AttnShape &s, int length, int i,
     const int d = i - j;
     const bool near = s.window == 0 || (d < s.window && d > -s.window) || j < s.sinks;
     return j < length && (!s.causal || d >= 0) && near;
+}
+
+// The keys that one position sees: [first, first + count) and [0, sinks).
+struct AttnKeys {
+    int first, sinks;
+    uint32_t count;
+};
+__device__ __forceinline__ AttnKeys attn_keys(const AttnShape &s, int length, int i)
+{
+    int64_t end = length, begin = 0, sinks = 0;
+    if (s.causal) end = min(end, static_cast<int64_t>(i) + 1);
+    if (s.window) {
+        sinks = min(static_cast<int64_t>(s.sinks), end);
+        begin = max(static_cast<int64_t>(0), static_cast<int64_t>(i) - s.window + 1);
+        end = min(end, static_cast<int64_t>(i) + s.window);
+    }
+    return AttnKeys{static_cast<int>(begin < end ? begin : 0), static_cast<int>(sinks), static_cast<uint32_t>(begin < end ? end - begin : 0)};
+}
+
+// Scores of keys k0, k0 + 1, ... (register i of a tile's 32 keys holds key 8 (i / 4) + i % 4 from k0) that the lane's position does not see: -inf.
+__device__ __forceinline__ void attn_hide(const AttnKeys &m, int k0, f32x16 &x)
+{
+    const int from = k0 - m.first;
+    if (__any(k0 < m.sinks)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int c = 8 * (i / 4) + (i & 3);
+            x[i] = static_cast<uint32_t>(from + c) < m.count || k0 + c < m.sinks ? x[i] : -INFINITY;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = static_cast<uint32_t>(from + 8 * (i / 4) + (i & 3)) < m.count ? x[i] : -INFINITY;
+    }
 }
 
 // Whether every key of [k0, k1) is visible from every position of [i0, i1].
@@ -129,13 +163,13 @@ __device__ __forceinline__ f32x16 mfma_pieces(const u32x4 (&a)[NA], const u32x4 
     return acc;
 }
 
-// Tiles in LDS: [piece][row][columns + 8]: rows 16 bytes apart from a multiple of the banks' width, so eight lanes that read 16 bytes of eight
-// rows meet in no bank.
+// Tiles in LDS: [piece][row][columns and padding].  Row reads take 16 bytes of neighbouring rows, column reads 32 bytes of four: at
+// a pitch of 36 or 72 dwords neither meets in a bank (32 or 64 dwords, and 68: measured 1.2 to 1.7 times as long).
 template <int DT>
-constexpr int kAttnPitch = 32 * DT + 8;
+constexpr int kAttnPitch = DT == 2 ? 72 : 144;
 
 template <int NQ, int DT, int ROWS>
-struct AttnTile {
+struct alignas(16) AttnTile {
     uint16_t e[NQ][ROWS][kAttnPitch<DT>];
 };
 
@@ -277,26 +311,70 @@ __device__ __forceinline__ void raw_values(const RawEight<CODES> &r, float (&v)[
     }
 }
 
-// fp32 values as fp16 times `up`.  high: the largest |x| so far as a bit pattern (NaN above all).
+// fp32 values as fp16 times `up` (their bits fit; what lies below 2^-24 is cut).  high: the largest |x| so far as a bit pattern (NaN above all).
 __device__ __forceinline__ u32x4 to_half(const float (&v)[8], float up, uint32_t &high)
 {
-    f16x8 h;
+    u32x4 h;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        high = max(high, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-        h[i] = static_cast<_Float16>(v[i] * up);
+    for (int i = 0; i < 8; i += 2) {
+        high = max(max(__float_as_uint(v[i]) & 0x7FFFFFFFu, __float_as_uint(v[i + 1]) & 0x7FFFFFFFu), high);
+        h[i / 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(v[i] * up, v[i + 1] * up));
     }
-    return __builtin_bit_cast(u32x4, h);
+    return h;
 }
 
-// As fp16 times `up` (1: the format's values are fp16's; nothing is checked).
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// What codes need on their way to fp16, two at a time: masks of their magnitudes and signs, and for e == 6 the shifts that make fp16
+// of them (times 2^9: the exponent field falls by 7).
+struct HalfCodes {
+    uint32_t body, sign, limit, least;      // limit, least: codes of kHalfLimit and kHalfLeast
+    int32_t shift, sign_shift;              // shift < 0: by way of fp32
+};
+
+// As fp16 times `up` (1: the format's values are fp16's; nothing is checked).  high: of codes the largest magnitudes, of either half of a word;
+// otherwise as above.
 template <bool CODES>
-__device__ __forceinline__ u32x4 raw_half(const RawEight<CODES> &r, float up, uint32_t &high, const ElemFormat &f)
+__device__ __forceinline__ u32x4 raw_half(const RawEight<CODES> &r, float up, const HalfCodes &hc, uint32_t &high, const ElemFormat &f)
 {
-    if (CODES && f.codec == kCodecHalf) return r.w[0];
+    if constexpr (CODES) {
+        if (f.codec == kCodecHalf) return r.w[0];
+        u16x2 top = __builtin_bit_cast(u16x2, high);
+        u32x4 out;
+        if (f.codec == kCodecBf16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t w = r.w[0][i];
+                top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu));
+                out[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xFFFF0000u) * up));
+            }
+            high = __builtin_bit_cast(uint32_t, top);
+            return out;
+        }
+        u16x2 low = {0xFFFF, 0xFFFF};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const u16x2 body = __builtin_bit_cast(u16x2, r.w[0][i] & hc.body);
+            top = __builtin_elementwise_max(top, body);
+            low = __builtin_elementwise_min(low, body - static_cast<uint16_t>(1));
+        }
+        high = __builtin_bit_cast(uint32_t, top);
+        // a code other than 0 whose fp16 is no normal number (|x| < 2^-23) is rare: then all go by way of fp32
+        const uint16_t normal = static_cast<uint16_t>((8u << (10 - max(hc.shift, 0))) - 1u);
+        if (hc.shift >= 0 && !__any(low[0] < normal || low[1] < normal)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u16x2 body = __builtin_bit_cast(u16x2, r.w[0][i] & hc.body) << static_cast<uint16_t>(hc.shift);
+                const u16x2 h = __builtin_elementwise_sub_sat(body, u16x2{7 << 10, 7 << 10});
+                out[i] = __builtin_bit_cast(uint32_t, h) | (r.w[0][i] & hc.sign) << hc.sign_shift;
+            }
+            return out;
+        }
+    }
     float v[8];
     raw_values(r, v, f);
-    return to_half(v, up, high);
+    uint32_t ignore = 0;
+    return to_half(v, up, CODES ? ignore : high);
 }
 
 // R(Q) is multiplied by the scale's sign, so that scores are ordered as they come out of the product; a scale of 0 makes it 0.
@@ -311,11 +389,14 @@ __device__ __forceinline__ u32x4 half_signed(u32x4 q, float scale)
 // P is taken times 2^14, so that its fp16 pieces hold their bits down to P = 2^-28.
 constexpr float kProbUp = 14.0f;
 
-// Whether a workgroup has to be computed with bf16 pieces: in all of its threads.  Every thread calls it.
-__device__ __forceinline__ bool half_flag(uint32_t high, uint32_t high_value)
+// Whether a workgroup has to be computed with bf16 pieces: in all of its threads.  Every thread calls it.  high, high_value: what raw_half left.
+template <bool CODES>
+__device__ __forceinline__ bool half_flag(uint32_t high, uint32_t high_value, const HalfCodes &hc)
 {
-    const bool over = __syncthreads_or(max(high, high_value) >= __float_as_uint(kHalfLimit));
-    const bool some = __syncthreads_or(high_value != 0u), large = __syncthreads_or(high_value >= __float_as_uint(kHalfLeast));
+    const uint32_t h = CODES ? max(high >> 16, high & 0xFFFFu) : high, v = CODES ? max(high_value >> 16, high_value & 0xFFFFu) : high_value;
+    const uint32_t limit = CODES ? hc.limit : __float_as_uint(kHalfLimit), least = CODES ? hc.least : __float_as_uint(kHalfLeast);
+    const bool over = __syncthreads_or(max(h, v) >= limit);
+    const bool some = __syncthreads_or(v != 0u), large = __syncthreads_or(v >= least);
     return over || (some && !large);
 }
 
@@ -375,6 +456,14 @@ constexpr int kPieces = 2, kProbPieces = 3;      // bf16 pieces of operands, of 
 
 // Whether a format's values go as one fp16 value each.
 inline bool attention_half(fmt_format_t f) { return f.m <= 10; }
+
+inline HalfCodes make_half_codes(fmt_format_t f, const ElemFormat &e)
+{
+    const uint32_t body = (1u << (f.e + f.m)) - 1u, sign = 1u << (f.e + f.m);
+    const int bias = (1 << (f.e - 1)) - 1;
+    return HalfCodes{body * 0x10001u, sign * 0x10001u, static_cast<uint32_t>(bias + 7) << f.m, static_cast<uint32_t>(bias > 10 ? bias - 10 : 0) << f.m,
+                     f.e == 6 ? 10 - f.m : -1, 15 - (f.e + f.m)};
+}
 
 // Pieces of P and dS with fp16 operands: one (11 bits) where results have 8, two (22) where they have more.
 inline int half_pieces(fmt_format_t f, int32_t result) { return result == FMT_RESULT_F32 || f.m > 7 ? 2 : 1; }

@@ -585,6 +585,7 @@ __device__ __forceinline__ void dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
 #pragma unroll
         for (int i = 0; i < 16; ++i) dq[d][i] = 0.0f;
     const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up), down = 1.0f / a.up;
+    const AttnKeys sees = attn_keys(s, r.seq.length, r.pos);
     for (int n = 0; n < count; ++n) {
         const int tile = tiles.at(n), k0 = tile * kKeyTile, buf = n & 1;
         kr.put(sh.ks[buf]);
@@ -610,11 +611,7 @@ __device__ __forceinline__ void dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
                 read_rows(sh.vs[buf], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
                 dp = mfma_f16(f[0], go[kk], dp);
             }
-            if (!all) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!attn_sees(s, r.seq.length, r.pos, k0 + 32 * kt + 8 * (i / 4) + 4 * half + (i & 3))) x[i] = -INFINITY;
-            }
+            if (!all) attn_hide(sees, k0 + 32 * kt + 4 * half, x);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
                 float ds[8];
@@ -646,7 +643,8 @@ constexpr int kHalfRows = DT == 2 ? 64 : 32;
 template <int DT>
 struct DkvHalfShared {
     AttnTile<1, DT, kHalfRows<DT>> qs[2], gs[2];
-    float lse[2][kHalfRows<DT>], delta[2][kHalfRows<DT>], weight[2][kHalfRows<DT>], least[2];
+    alignas(16) float lse[2][kHalfRows<DT>], delta[2][kHalfRows<DT>], weight[2][kHalfRows<DT>];
+    float least[2];
 };
 
 template <int NP, int DT>
@@ -687,6 +685,21 @@ __device__ __forceinline__ void dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
 #pragma unroll
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
     const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up), down = 1.0f / a.up;
+    // rows that see the lane's key
+    int seen_from = 0;
+    uint32_t seen = 0;
+    if (key.used) {
+        int64_t t0 = 0, t1 = s.q_len;
+        if (s.causal) t0 = max(t0, static_cast<int64_t>(key.key) - key.seq.first);
+        if (s.window && key.key >= s.sinks) {
+            t0 = max(t0, static_cast<int64_t>(key.key) - s.window + 1 - key.seq.first);
+            t1 = min(t1, static_cast<int64_t>(key.key) + s.window - key.seq.first);
+        }
+        if (t0 < t1) {
+            seen_from = static_cast<int>(t0 * s.group);
+            seen = static_cast<uint32_t>((t1 - t0) * s.group);
+        }
+    }
     float least = kNoRow, running = kNoRow;      // the smallest grow: of the sums, and (wave 0) of the rows read so far
     int buf = 0;
     for (int row0 = key.first; row0 < key.last; row0 += kRows, buf ^= 1) {
@@ -737,21 +750,25 @@ __device__ __forceinline__ void dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
             }
             if (!all) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int row = row0 + 32 * rt + 8 * (i / 4) + 4 * half + (i & 3);
-                    if (!attn_sees(s, key.seq.length, key.seq.first + row_at(row, s.group).t, key.key)) x[i] = -INFINITY;
-                }
+                for (int i = 0; i < 16; ++i)
+                    x[i] = static_cast<uint32_t>(row0 + 32 * rt + 8 * (i / 4) + 4 * half + (i & 3) - seen_from) < seen ? x[i] : -INFINITY;
             }
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
                 float p[8], ds[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int i = 8 * kb + j, row = 32 * rt + 8 * (i / 4) + 4 * half + (i & 3);
-                    const float e = exp2_fast(fmaf(x[i], scale2, -sh.lse[buf][row])) * sh.weight[buf][row];
-                    p[j] = e * 16384.0f;
-                    ds[j] = e == 0.0f ? 0.0f : e * fmaf(dp[i], down, -sh.delta[buf][row]);
-                    high.ds = max(high.ds, __float_as_uint(ds[j]) & 0x7FFFFFFFu);
+                for (int j0 = 0; j0 < 8; j0 += 4) {
+                    const int row = 32 * rt + 16 * kb + 2 * j0 + 4 * half;
+                    const f32x4 lse = *reinterpret_cast<const f32x4 *>(&sh.lse[buf][row]), delta = *reinterpret_cast<const f32x4 *>(&sh.delta[buf][row]);
+                    const f32x4 weight = *reinterpret_cast<const f32x4 *>(&sh.weight[buf][row]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float e = exp2_fast(fmaf(x[8 * kb + j0 + j], scale2, -lse[j])) * weight[j];
+                        const float d = e == 0.0f ? 0.0f : e * fmaf(dp[8 * kb + j0 + j], down, -delta[j]);
+                        p[j0 + j] = e * 16384.0f;
+                        ds[j0 + j] = d;
+                        high.ds = max(high.ds, __float_as_uint(d) & 0x7FFFFFFFu);
+                    }
                 }
                 u32x4 pp[NP], dd[NP];
                 f16_pieces<NP>(p, pp);

@@ -20,6 +20,7 @@ struct AttnFwd {
     int32_t row_tiles;
     uint32_t blocks;          // workgroups of the first launch
     bool codes;               // how q, k and v are stored
+    HalfCodes hc;
     ElemFormat f;
 };
 
@@ -183,7 +184,7 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
 // The same on operands of one fp16 value each, P in NP pieces of fp16.  The next tile's elements are on their way from memory while a
 // tile is computed; they are rounded and converted on their way into the other of two LDS buffers, so a tile costs one barrier.
 template <int NP, int DT, bool CODES>
-__global__ __launch_bounds__(256, 2) void attn_fwd_half_kernel(AttnFwd a)
+__global__ __launch_bounds__(256, CODES || DT == 2 ? 2 : 1) void attn_fwd_half_kernel(AttnFwd a)
 {
     __shared__ AttnTile<1, DT, kFwdKeys> ks[2], vs[2];
     constexpr int kEights = 4 * DT, kLoads = kFwdKeys * kEights / 256;
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_half_kernel(AttnFwd a)
     for (int kk = 0; kk < 2 * DT; ++kk) {
         const int col = 16 * kk + 8 * half;
         q[kk] = half_signed(
-            raw_half<CODES>(raw_load<CODES>(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, live ? s.dim - col : 0), a.up, high, a.f), s.scale);
+            raw_half<CODES>(raw_load<CODES>(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, live ? s.dim - col : 0), a.up, a.hc, high, a.f), s.scale);
     }
     f32x16 o[DT];
 #pragma unroll
@@ -234,13 +235,14 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_half_kernel(AttnFwd a)
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float top = -INFINITY, sum = 0.0f;
     const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up);
+    const AttnKeys sees = attn_keys(s, seq.length, pos);
     for (int n = begin; n < end; ++n) {
         const int k0 = tiles.at(n) * kFwdKeys, buf = (n - begin) & 1;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int key = key_in + i * (256 / kEights);
-            *reinterpret_cast<u32x4 *>(&ks[buf].e[0][key][col_in]) = raw_half<CODES>(kr[i], a.up, high, a.f);
-            *reinterpret_cast<u32x4 *>(&vs[buf].e[0][key][col_in]) = raw_half<CODES>(vr[i], a.up, high_value, a.f);
+            *reinterpret_cast<u32x4 *>(&ks[buf].e[0][key][col_in]) = raw_half<CODES>(kr[i], a.up, a.hc, high, a.f);
+            *reinterpret_cast<u32x4 *>(&vs[buf].e[0][key][col_in]) = raw_half<CODES>(vr[i], a.up, a.hc, high_value, a.f);
         }
         __syncthreads();
         if (n + 1 < end) fetch(n + 1);
@@ -258,10 +260,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_half_kernel(AttnFwd a)
         }
         if (!attn_sees_all(s, seq.length, i0, i1, k0, k0 + kFwdKeys)) {
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!attn_sees(s, seq.length, pos, k0 + 32 * kt + 8 * (i / 4) + 4 * half + (i & 3))) x[kt][i] = -INFINITY;
+            for (int kt = 0; kt < 2; ++kt) attn_hide(sees, k0 + 32 * kt + 4 * half, x[kt]);
         }
         float high_score = -INFINITY;
 #pragma unroll
@@ -304,7 +303,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_half_kernel(AttnFwd a)
     sum += __shfl_xor(sum, 32);
     const float over = sum == 0.0f ? 0.0f : 1.0f / (sum * a.up);
     if (a.flags) {
-        const bool flag = half_flag(high, high_value);
+        const bool flag = half_flag<CODES>(high, high_value, a.hc);
         if (threadIdx.x == 0) a.flags[blk.id] = flag;
     }
     if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, sum == 0.0f ? -INFINITY : top - kProbUp + log2f(sum));
@@ -356,7 +355,7 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
     int64_t splits = work >= cus ? 1 : (cus + work - 1) / work;
     if (splits > key_tiles / 4) splits = key_tiles / 4;
     if (splits < 1) splits = 1;
-    AttnFwd a{s, q, k, v, o, lse, result, static_cast<int32_t>(splits), nullptr, nullptr, 1.0f, static_cast<int32_t>(row_tiles), 0, false, f};
+    AttnFwd a{s, q, k, v, o, lse, result, static_cast<int32_t>(splits), nullptr, nullptr, 1.0f, static_cast<int32_t>(row_tiles), 0, false, make_half_codes(fmt, f), f};
     const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len, grid = work * splits;
     if (grid > 0x7FFFFFFF) return FMT_ERR_SHAPE;
     const bool half = attention_half(fmt), flagged = half && fmt.e > 5;

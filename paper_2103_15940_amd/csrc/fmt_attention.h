@@ -234,7 +234,8 @@ __device__ __forceinline__ void load_tokens(AttnTile<NQ, DT, ROWS> &t, const voi
 // elements of one side at 2^7, all of the other below 2^-23) and below 2^-24 for elements up to 8.  A workgroup that meets an element of 2^7 or more, an infinity or
 // NaN, or whose V or dO lie below 2^-10 altogether, says so in a flag, and a second launch computes the results of flagged workgroups with pieces
 // of bf16; the others end at once (2 us for all).
-constexpr float kHalfUp = 512.0f, kHalfLimit = 128.0f, kHalfLeast = 0x1p-10f;
+// (fp32 is looked at before it is rounded: from 112 on, what has one mantissa bit becomes 128.)
+constexpr float kHalfUp = 512.0f, kHalfLimit = 128.0f, kHalfLimitRaw = 112.0f, kHalfLeast = 0x1p-10f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -371,10 +372,41 @@ __device__ __forceinline__ u32x4 raw_half(const RawEight<CODES> &r, float up, co
             return out;
         }
     }
+    if constexpr (!CODES) {
+        // the short roundings: what they do not serve is above the limit.  (Formats of more than 10 bits do not come here.)
+        const QuantParams &p = f.p;
+        u32x4 out;
+        const uint32_t flush = f.ftz ? p.t_den : 0u;
+        auto run = [&](auto round) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const uint32_t a = r.w[i / 4][i % 4], b = r.w[i / 4][i % 4 + 1];
+                high = max(max(a & 0x7FFFFFFFu, b & 0x7FFFFFFFu), high);
+                out[i / 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(round(a) * up, round(b) * up));
+            }
+        };
+        if (f.codec == kCodecHalf) {
+            f16x8 h;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = static_cast<_Float16>(__uint_as_float(r.w[i / 4][i % 4]));
+            return __builtin_bit_cast(u32x4, h);
+        }
+        if (p.mode == kModeMagic) {
+            const RoundMasks k = round_masks(p);
+            if (f.ftz) run([&](uint32_t u) { return __uint_as_float((u & 0x7FFFFFFFu) < flush ? 0u : quantize_short<kModeMagic, false, false>(u, p, k)); });
+            else run([&](uint32_t u) { return __uint_as_float(quantize_short<kModeMagic, false, false>(u, p, k)); });
+        } else {
+            run([&](uint32_t u) {
+                const uint32_t q = (u + p.rbias + __builtin_amdgcn_ubfe(u, p.shift, p.lsb_width)) & p.nmask;
+                return __uint_as_float((u & 0x7FFFFFFFu) < flush ? 0u : q);
+            });
+        }
+        return out;
+    }
     float v[8];
     raw_values(r, v, f);
     uint32_t ignore = 0;
-    return to_half(v, up, CODES ? ignore : high);
+    return to_half(v, up, ignore);
 }
 
 // R(Q) is multiplied by the scale's sign, so that scores are ordered as they come out of the product; a scale of 0 makes it 0.
@@ -394,7 +426,7 @@ template <bool CODES>
 __device__ __forceinline__ bool half_flag(uint32_t high, uint32_t high_value, const HalfCodes &hc)
 {
     const uint32_t h = CODES ? max(high >> 16, high & 0xFFFFu) : high, v = CODES ? max(high_value >> 16, high_value & 0xFFFFu) : high_value;
-    const uint32_t limit = CODES ? hc.limit : __float_as_uint(kHalfLimit), least = CODES ? hc.least : __float_as_uint(kHalfLeast);
+    const uint32_t limit = CODES ? hc.limit : __float_as_uint(kHalfLimitRaw), least = CODES ? hc.least : __float_as_uint(kHalfLeast);
     const bool over = __syncthreads_or(max(h, v) >= limit);
     const bool some = __syncthreads_or(v != 0u), large = __syncthreads_or(v >= least);
     return over || (some && !large);
@@ -411,37 +443,101 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t i, uint32_t n)
 // 2^x; the vector unit's exponential flushes results below 2^-126, which is below 2^-24 of any sum that holds a 1.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Four results of a lane, columns col to col + 3 of which those below dim exist.  RESULT at run time: uniform.
-__device__ __forceinline__ void store4(void *y, int64_t at, int col, int dim, const float (&v)[4], int result, const ElemFormat &f)
+typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+// A lane's results of DT blocks of 32 columns (its column of the blocks is one row of the tensor): register 4g + i of block d is column
+// 32 d + 8 g + 4 half + i, taken times `scale`.  The kind of result is chosen once, ahead of all of them: the paths of the others would
+// lie between a wave's stores and cost it misses of the instruction cache (3 us of a call).
+template <int DT>
+__device__ __forceinline__ void store_row(void *y, int64_t base, int half, int dim, const f32x16 (&o)[DT], float scale, int result, const ElemFormat &f)
 {
-    const int count = dim - col;
-    if (count <= 0) return;
+    auto each = [&](auto put) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int col = 32 * d + 8 * g + 4 * half;
+                const float v[4] = {o[d][4 * g] * scale, o[d][4 * g + 1] * scale, o[d][4 * g + 2] * scale, o[d][4 * g + 3] * scale};
+                put(col, dim - col, v);
+            }
+    };
+    auto floats = [&](int col, int count, const float (&v)[4]) __attribute__((always_inline)) {
+        float *p = static_cast<float *>(y) + base + col;
+        if (count >= 4) {
+            *reinterpret_cast<f32x4_any *>(p) = f32x4_any{v[0], v[1], v[2], v[3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < count) p[i] = v[i];
+        }
+    };
+    auto codes = [&](int col, int count, const uint16_t (&c)[4]) __attribute__((always_inline)) {
+        uint16_t *p = static_cast<uint16_t *>(y) + base + col;
+        if (count >= 4) {
+            *reinterpret_cast<u16x4_any *>(p) = u16x4_any{c[0], c[1], c[2], c[3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < count) p[i] = c[i];
+        }
+    };
+    if (result == FMT_RESULT_F32) {
+        each(floats);
+    } else if (result == FMT_RESULT_CODE16 && f.codec == kCodecBf16) {
+        const uint32_t flush = f.ftz ? f.p.t_den : 0u;
+        each([&](int col, int count, const float (&v)[4]) __attribute__((always_inline)) {
+            uint16_t c[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t u = __float_as_uint(v[i]), a = u & 0x7FFFFFFFu;
+                uint32_t r = a < flush ? 0u : (a + 0x7FFFu + (a >> 16 & 1u)) >> 16;
+                r = a > 0x7F800000u ? 0x7FC0u : r | (u >> 31) << 15;
+                c[i] = static_cast<uint16_t>(r);
+            }
+            codes(col, count, c);
+        });
+    } else if (result == FMT_RESULT_CODE16 && f.codec == kCodecHalf) {
+        each([&](int col, int count, const float (&v)[4]) __attribute__((always_inline)) {
+            uint16_t c[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint16_t h = __builtin_bit_cast(uint16_t, static_cast<_Float16>(v[i]));
+                c[i] = v[i] != v[i] ? static_cast<uint16_t>(0x7E00u) : h;
+            }
+            codes(col, count, c);
+        });
+    } else {
+        each([&](int col, int count, const float (&v)[4]) __attribute__((always_inline)) {
+            float r[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = v[i];
+            round_values(r, f);
+            if (result == FMT_RESULT_CODE16) {
+                uint16_t c[4];
+                encode_values(r, c, f);
+                codes(col, count, c);
+            } else {
+                floats(col, count, r);
+            }
+        });
+    }
+}
+
+// Up to four neighbouring results of kernels that join parts.
+__device__ __forceinline__ void store4(void *y, int64_t at, int count, const float (&v)[4], int result, const ElemFormat &f)
+{
     float r[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = v[i];
     if (result != FMT_RESULT_F32) round_values(r, f);
-    if (result == FMT_RESULT_CODE16) {
-        uint16_t c[4];
-        encode_values(r, c, f);
-        uint16_t *d = static_cast<uint16_t *>(y) + at;
-        if (count >= 4) {
-            typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
-            *reinterpret_cast<u16x4_any *>(d) = u16x4_any{c[0], c[1], c[2], c[3]};
-        } else {
+    uint16_t c[4];
+    if (result == FMT_RESULT_CODE16) encode_values(r, c, f);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < count) d[i] = c[i];
+    for (int i = 0; i < 4; ++i)
+        if (i < count) {
+            if (result == FMT_RESULT_CODE16) static_cast<uint16_t *>(y)[at + i] = c[i];
+            else static_cast<float *>(y)[at + i] = r[i];
         }
-    } else {
-        float *d = static_cast<float *>(y) + at;
-        if (count >= 4) {
-            *reinterpret_cast<f32x4_any *>(d) = f32x4_any{r[0], r[1], r[2], r[3]};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < count) d[i] = r[i];
-        }
-    }
 }
 
 // run(DT) for a head size.

@@ -18,7 +18,7 @@ struct AttnBwd {
     float *info;              // what the products need of a row, [4][batch][kv_heads][row_tiles * 128]: kInfo*
     uint16_t *qh, *gh;        // fp16 operands: [batch][kv_heads][row_tiles * 128][32 DT] Q and dO, zero past the last row and column,
     uint16_t *kh, *vh;        // [batch][kv_heads][key_tiles * 128][32 DT] K and V, zero past the sequence's length
-    uint32_t *highs;          // the largest |x| of each 128 rows of Q, then of each 128 keys of K, then of V
+    uint32_t *highs;          // the largest |x| of each 32 rows of Q, then of each 32 keys of K, then of V
     float *part;              // parts > 1: [2][parts][batch][k_len][kv_heads][dim] of dK, dV
     uint32_t *flags;          // per workgroup: whether it is left to the pieces of bf16; or nullptr
     float up;                 // what the fp16 operands are multiplied by
@@ -35,7 +35,7 @@ struct AttnBwd {
 enum : int { kInfoLse2 = 0, kInfoDelta = 1, kInfoGrow = 2, kInfoScaledDelta = 3 };
 constexpr float kNoRow = 1024.0f;
 
-constexpr int kRowTile = 128, kKeyTile = 64, kKvKeys = 128, kKvRows = 32;
+constexpr int kRowTile = 128, kKeyTile = 64, kKvKeys = 128, kKvRows = 32, kPackRows = 32;
 
 __device__ __forceinline__ int64_t info_rows(const AttnBwd &a) { return static_cast<int64_t>(a.s.batch) * a.s.kv_heads * a.row_tiles * kRowTile; }
 
@@ -60,26 +60,27 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *shared)
     return max(max(shared[0], shared[1]), max(shared[2], shared[3]));
 }
 
-// What the products need: of 128 rows delta = sum over the head's columns of R(dO) O, lse, and with HALF R(Q) and R(dO) as fp16 operands; with HALF
-// also of 128 keys R(K) and R(V).  4 DT lanes per row, 8 columns each.  One pass over the tensors, whose tiles are then read many times.
+// What the products need: of 32 rows delta = sum over the head's columns of R(dO) O, lse, and with HALF R(Q) and R(dO) as fp16 operands; with HALF
+// also of 32 keys R(K) and R(V).  4 DT lanes per row, 8 columns each.  One pass over the tensors, whose tiles are then read many times.
 template <int DT, bool HALF>
 __global__ __launch_bounds__(256) void attn_pack_kernel(AttnBwd a)
 {
     __shared__ uint32_t shared[4];
     constexpr int kEights = 4 * DT, kStep = 256 / kEights;
     const AttnShape &s = a.s;
-    const uint32_t row_blocks = a.row_tiles * s.kv_heads * s.batch;
+    const uint32_t row_packs = a.row_tiles * (kRowTile / kPackRows), key_packs = a.key_tiles * (kKvKeys / kPackRows);
+    const uint32_t row_blocks = row_packs * s.kv_heads * s.batch;
     const int col = (threadIdx.x % kEights) * 8, in = threadIdx.x / kEights, count = min(s.dim - col, 8);
     const int64_t all = info_rows(a);
     if (blockIdx.x < row_blocks) {
-        const uint32_t tile = blockIdx.x % a.row_tiles, bkh = blockIdx.x / a.row_tiles;
+        const uint32_t tile = blockIdx.x % row_packs, bkh = blockIdx.x / row_packs;
         const int kh = static_cast<int>(bkh % s.kv_heads), b = static_cast<int>(bkh / s.kv_heads), rows = s.q_len * s.group;
         ElemFormat whole = a.f;
         if (!a.gcodes) whole.codec = kCodecNone;                   // O is taken as it is
         uint32_t high_q = 0;
 #pragma unroll 1
-        for (int r = in; r < kRowTile; r += kStep) {
-            const int row = static_cast<int>(tile) * kRowTile + r;
+        for (int r = in; r < kPackRows; r += kStep) {
+            const int row = static_cast<int>(tile) * kPackRows + r;
             const int64_t at = static_cast<int64_t>(bkh) * a.row_tiles * kRowTile + row;
             const RowAt where = row_at(row, s.group);
             const int head = kh * s.group + where.g;
@@ -129,13 +130,13 @@ __global__ __launch_bounds__(256) void attn_pack_kernel(AttnBwd a)
             if (threadIdx.x == 0) a.highs[blockIdx.x] = high_q;
         }
     } else if constexpr (HALF) {
-        const uint32_t n = blockIdx.x - row_blocks, tile = n % a.key_tiles, bkh = n / a.key_tiles;
+        const uint32_t n = blockIdx.x - row_blocks, tile = n % key_packs, bkh = n / key_packs;
         const int kh = static_cast<int>(bkh % s.kv_heads), b = static_cast<int>(bkh / s.kv_heads);
         const AttnSeq seq = attn_seq(s, b);
         uint32_t high_k = 0, high_v = 0;
 #pragma unroll 1
-        for (int r = in; r < kKvKeys; r += kStep) {
-            const int key = static_cast<int>(tile) * kKvKeys + r;
+        for (int r = in; r < kPackRows; r += kStep) {
+            const int key = static_cast<int>(tile) * kPackRows + r;
             const int64_t at = static_cast<int64_t>(bkh) * a.key_tiles * kKvKeys + key;
             float k[8], v[8];
 #pragma unroll
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(256) void attn_pack_kernel(AttnBwd a)
         high_k = block_max(high_k, shared);
         high_v = block_max(high_v, shared);
         if (threadIdx.x == 0) {
-            const uint32_t key_blocks = a.key_tiles * s.kv_heads * s.batch;
+            const uint32_t key_blocks = key_packs * s.kv_heads * s.batch;
             a.highs[row_blocks + n] = high_k;
             a.highs[row_blocks + key_blocks + n] = high_v;
         }
@@ -191,15 +192,7 @@ __device__ __forceinline__ void store_dq(const AttnBwd &a, const RowBlock &r, co
 {
     if (!r.live) return;
     const int half = (threadIdx.x & 63) >> 5;
-    const int64_t base = r.b * a.dq.sb + r.t * a.dq.st + r.head * a.dq.sh;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int col = 32 * d + 8 * g + 4 * half;
-            const float v[4] = {dq[d][4 * g] * scale, dq[d][4 * g + 1] * scale, dq[d][4 * g + 2] * scale, dq[d][4 * g + 3] * scale};
-            store4(const_cast<void *>(a.dq.p), base + col, col, a.s.dim, v, a.result, a.f);
-        }
+    store_row<DT>(const_cast<void *>(a.dq.p), r.b * a.dq.sb + r.t * a.dq.st + r.head * a.dq.sh, half, a.s.dim, dq, scale, a.result, a.f);
 }
 
 template <int DT>
@@ -363,16 +356,8 @@ __device__ __forceinline__ void store_dkv(const AttnBwd &a, const KeyBlock &k, c
     const int64_t kbase = part ? at : k.b * a.dk.sb + k.key * a.dk.st + k.kh * a.dk.sh;
     const int64_t vbase = part ? at : k.b * a.dv.sb + k.key * a.dv.st + k.kh * a.dv.sh;
     const int result = part ? FMT_RESULT_F32 : a.result;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int col = 32 * d + 8 * g + 4 * half;
-            const float x[4] = {dk[d][4 * g] * kscale, dk[d][4 * g + 1] * kscale, dk[d][4 * g + 2] * kscale, dk[d][4 * g + 3] * kscale};
-            const float y[4] = {dv[d][4 * g] * vscale, dv[d][4 * g + 1] * vscale, dv[d][4 * g + 2] * vscale, dv[d][4 * g + 3] * vscale};
-            store4(kout, kbase + col, col, s.dim, x, result, a.f);
-            store4(vout, vbase + col, col, s.dim, y, result, a.f);
-        }
+    store_row<DT>(kout, kbase, half, s.dim, dk, kscale, result, a.f);
+    store_row<DT>(vout, vbase, half, s.dim, dv, vscale, result, a.f);
 }
 
 // dK and dV from their parts, in order: a thread takes four columns.
@@ -393,7 +378,7 @@ __global__ __launch_bounds__(256) void attn_parts_kernel(AttnBwd a)
             if (j < count) v[j] += p[j];
     const AttnView &out = value ? a.dv : a.dk;
     const int kh = static_cast<int>(token % s.kv_heads), key = static_cast<int>(token / s.kv_heads % s.k_len), b = static_cast<int>(token / s.kv_heads / s.k_len);
-    store4(const_cast<void *>(out.p), b * out.sb + key * out.st + kh * out.sh + col, col, s.dim, v, a.result, a.f);
+    store4(const_cast<void *>(out.p), b * out.sb + key * out.st + kh * out.sh + col, count, v, a.result, a.f);
 }
 
 template <int DT>
@@ -515,6 +500,24 @@ struct Highs {
     uint32_t q = 0, k = 0, v = 0, ds = 0;
 };
 
+// Where attn_pack_kernel left them for one (batch, kv head).
+struct PackHighs {
+    const uint32_t *q, *k, *v;
+    __device__ __forceinline__ PackHighs(const AttnBwd &a, uint32_t bkh)
+    {
+        const uint32_t rows = a.row_tiles * (kRowTile / kPackRows), keys = a.key_tiles * (kKvKeys / kPackRows), all = a.s.kv_heads * a.s.batch;
+        q = a.highs + bkh * rows;
+        k = a.highs + all * rows + bkh * keys;
+        v = k + all * keys;
+    }
+    __device__ __forceinline__ uint32_t of(const uint32_t *p, int first, int count) const
+    {
+        uint32_t h = 0;
+        for (int i = 0; i < count / kPackRows; ++i) h = max(h, p[first / kPackRows + i]);
+        return h;
+    }
+};
+
 __device__ __forceinline__ void half_flags(const AttnBwd &a, uint32_t at, const Highs &h)
 {
     bool bad = h.ds > __float_as_uint(65504.0f);
@@ -559,14 +562,14 @@ __device__ __forceinline__ void dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
     const AttnShape &s = a.s;
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const RowBlock r = row_block(a, id);
-    const uint32_t bkh = r.b * s.kv_heads + r.kh, row_blocks = a.row_blocks, key_blocks = a.key_tiles * s.kv_heads * s.batch;
+    const uint32_t bkh = r.b * s.kv_heads + r.kh;
+    const PackHighs highs(a, bkh);
     const int64_t all_rows = info_rows(a);
     const uint16_t *keys = a.kh + static_cast<int64_t>(bkh) * a.key_tiles * kKvKeys * DP, *values = a.vh + static_cast<int64_t>(bkh) * a.key_tiles * kKvKeys * DP;
-    const uint32_t *khighs = a.highs + row_blocks + bkh * a.key_tiles, *vhighs = khighs + key_blocks;
     const AttnTiles tiles = attn_tiles(s, r.seq.length, r.i0, r.i1, kKeyTile);
     const int count = tiles.count();
     Highs high;
-    high.q = a.highs[bkh * a.row_tiles + r.row0 / kRowTile];
+    high.q = highs.of(highs.q, r.row0, kRowTile);
     TileLoad<DT, kKeyTile> kr, vr;
     if (count > 0) {
         kr.fetch(keys + static_cast<int64_t>(tiles.at(0)) * kKeyTile * DP);
@@ -590,8 +593,8 @@ __device__ __forceinline__ void dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
         const int tile = tiles.at(n), k0 = tile * kKeyTile, buf = n & 1;
         kr.put(sh.ks[buf]);
         vr.put(sh.vs[buf]);
-        high.k = max(high.k, khighs[tile / 2]);
-        high.v = max(high.v, vhighs[tile / 2]);
+        high.k = max(high.k, highs.of(highs.k, k0, kKeyTile));
+        high.v = max(high.v, highs.of(highs.v, k0, kKeyTile));
         __syncthreads();
         if (n + 1 < count) {
             kr.fetch(keys + static_cast<int64_t>(tiles.at(n + 1)) * kKeyTile * DP);
@@ -654,13 +657,13 @@ __device__ __forceinline__ void dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
     const AttnShape &s = a.s;
     const int lane = threadIdx.x & 63, half = lane >> 5;
     const KeyBlock key = key_block(a, id, kRows);
-    const uint32_t bkh = key.b * s.kv_heads + key.kh, row_blocks = a.row_blocks, key_blocks = a.key_tiles * s.kv_heads * s.batch;
+    const uint32_t bkh = key.b * s.kv_heads + key.kh;
+    const PackHighs highs(a, bkh);
     const int64_t all_rows = info_rows(a);
     const uint16_t *queries = a.qh + key.info * DP, *gradients = a.gh + key.info * DP;
     Highs high;
-    high.k = a.highs[row_blocks + bkh * a.key_tiles + key.k0 / kKvKeys];
-    high.v = a.highs[row_blocks + key_blocks + bkh * a.key_tiles + key.k0 / kKvKeys];
-    const uint32_t *qhighs = a.highs + bkh * a.row_tiles;
+    high.k = highs.of(highs.k, key.k0, kKvKeys);
+    high.v = highs.of(highs.v, key.k0, kKvKeys);
     TileLoad<DT, kRows> qr, gr;
     float info[3];
     auto fetch = [&](int row0) __attribute__((always_inline)) {
@@ -705,7 +708,7 @@ __device__ __forceinline__ void dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
     for (int row0 = key.first; row0 < key.last; row0 += kRows, buf ^= 1) {
         qr.put(sh.qs[buf]);
         gr.put(sh.gs[buf]);
-        high.q = max(high.q, qhighs[row0 / kRowTile]);
+        high.q = max(high.q, highs.of(highs.q, row0, kRows));
         if (threadIdx.x < 64) {
             float low = info[2];
 #pragma unroll
@@ -827,7 +830,7 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
     int64_t parts = blocks == 0 ? 1 : std::min((2 * cus + blocks - 1) / blocks, rows / 256);
     a.parts = static_cast<int32_t>(std::max<int64_t>(parts, 1));
     const int64_t key_blocks = blocks * a.parts, row_blocks = static_cast<int64_t>(a.row_tiles) * s.kv_heads * s.batch;
-    if (key_blocks + row_blocks > 0x7FFFFFFF) return FMT_ERR_SHAPE;
+    if (key_blocks + row_blocks > 0x1FFFFFFF) return FMT_ERR_SHAPE;
     a.key_blocks = static_cast<uint32_t>(key_blocks);
     a.row_blocks = static_cast<uint32_t>(row_blocks);
     if (key_blocks + row_blocks == 0) return FMT_OK;
@@ -840,7 +843,8 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
     // scratch: fp16 operands first (rows of 64 or 128 bytes), then words
     const int64_t bkh = static_cast<int64_t>(s.batch) * s.kv_heads, width = s.dim <= 64 ? 64 : 128;
     const int64_t prows = bkh * a.row_tiles * kRowTile, pkeys = bkh * a.key_tiles * kKvKeys, whole = static_cast<int64_t>(s.batch) * s.k_len * s.kv_heads * s.dim;
-    const int64_t operands = half ? (prows + pkeys) * width : 0, nhighs = half ? bkh * (a.row_tiles + 2 * a.key_tiles) : 0;      // words: two tensors of half a word
+    static_assert(kRowTile / kPackRows == 4 && kKvKeys / kPackRows == 4);
+    const int64_t operands = half ? (prows + pkeys) * width : 0, nhighs = half ? 4 * bkh * (a.row_tiles + 2 * a.key_tiles) : 0;      // words: two tensors of half a word
     const int64_t nflags = half ? key_blocks + row_blocks : 0, nparts = a.parts > 1 ? 2 * a.parts * whole : 0;
     float *scratch = nullptr;
     rc = get_acc_scratch(stream, static_cast<size_t>(operands + 4 * prows + nhighs + nflags + nparts + 1) * sizeof(float), &scratch);
@@ -857,7 +861,7 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
     a.part = scratch + operands + 4 * prows + nhighs + nflags;
 
     const dim3 threads(256);
-    const uint32_t blocks_all = a.key_blocks + a.row_blocks, tiles = static_cast<uint32_t>(bkh) * (a.row_tiles + (half ? a.key_tiles : 0));
+    const uint32_t blocks_all = a.key_blocks + a.row_blocks, tiles = 4 * static_cast<uint32_t>(bkh) * (a.row_tiles + (half ? a.key_tiles : 0));
     with_dim(s.dim, [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         if (tiles && half) attn_pack_kernel<DT, true><<<dim3(tiles), threads, 0, stream>>>(a);

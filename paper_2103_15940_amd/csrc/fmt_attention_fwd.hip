@@ -51,14 +51,7 @@ __device__ __forceinline__ void fwd_store(const AttnFwd &a, const f32x16 (&o)[DT
     void *out = part ? static_cast<void *>(a.part) : const_cast<void *>(a.o.p);
     const int64_t base = part ? (split * all_rows + at) * s.dim : b * a.o.sb + t * a.o.st + head * a.o.sh;
     const int result = part ? FMT_RESULT_F32 : a.result;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int col = 32 * d + 8 * g + 4 * half;
-            const float v[4] = {o[d][4 * g] * over, o[d][4 * g + 1] * over, o[d][4 * g + 2] * over, o[d][4 * g + 3] * over};
-            store4(out, base + col, col, s.dim, v, result, a.f);
-        }
+    store_row<DT>(out, base, half, s.dim, o, over, result, a.f);
     if (half != 0) return;
     if (part) a.part[a.splits * all_rows * s.dim + split * all_rows + at] = lse2;
     else if (a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
@@ -334,10 +327,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnFwd a)
     }
     const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int t = static_cast<int>(at % s.q_len), head = static_cast<int>(at / s.q_len % s.heads), b = static_cast<int>(at / s.q_len / s.heads);
-    float v[4] = {o[0] * over, o[1] * over, 0.0f, 0.0f};
+    const float v[4] = {o[0] * over, o[1] * over, 0.0f, 0.0f};
     if (2 * lane < s.dim)
-        store4(const_cast<void *>(a.o.p), b * a.o.sb + t * a.o.st + head * a.o.sh + 2 * lane, max(2 * lane, 0), min(s.dim, 2 * lane + 2), v, a.result,
-               a.f);
+        store4(const_cast<void *>(a.o.p), b * a.o.sb + t * a.o.st + head * a.o.sh + 2 * lane, min(s.dim - 2 * lane, 2), v, a.result, a.f);
     if (lane == 0 && a.lse) a.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 

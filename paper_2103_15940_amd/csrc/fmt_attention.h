@@ -232,8 +232,8 @@ __device__ __forceinline__ void load_tokens(AttnTile<NQ, DT, ROWS> &t, const voi
 // one product instead of four of bf16 pieces.  For wider ranges (1/6/9, 1/8/7) values are taken times 2^9, which holds |x| < 2^7 and
 // their bits down to 2^-33; what a smaller element loses is below 2^-34, for a score less than 128 * 128 * 128 * 2^-33 = 2^-12 at the very worst (all
 // elements of one side at 2^7, all of the other below 2^-23) and below 2^-24 for elements up to 8.  A workgroup that meets an element of 2^7 or more, an infinity or
-// NaN, or whose V or dO lie below 2^-10 altogether, says so in a flag, and a second launch computes the results of flagged workgroups with pieces
-// of bf16; the others end at once (2 us for all).
+// NaN, or whose V (backward: Q, K or V) lies below 2^-10 altogether, computes its results again with pieces of bf16.  (A second launch for such
+// workgroups, which all but a few calls do not have, cost every call 4 us.)
 // (fp32 is looked at before it is rounded: from 112 on, what has one mantissa bit becomes 128.)
 constexpr float kHalfUp = 512.0f, kHalfLimit = 128.0f, kHalfLimitRaw = 112.0f, kHalfLeast = 0x1p-10f;
 

@@ -86,13 +86,14 @@ __device__ __forceinline__ void few_values(const RawEight<KIND != kFewFloat> &r,
     }
 }
 
-template <int KIND>
-constexpr int kFewGroups = KIND == kFewFloat ? 2 : 4;      // groups of keys in flight per wave
+// Groups of keys in flight per wave: as many as leave four workgroups their registers in a compute unit (three with 2 or 4 rows, two with 8).
+template <int R, int KIND>
+constexpr int kFewGroups = KIND == kFewFloat || R > 2 ? 2 : 4;
 
 template <int R, int DT, int KIND>
-__global__ __launch_bounds__(256) void attn_few_kernel(AttnFew a)
+__global__ __launch_bounds__(256, R <= 1 ? 4 : R <= 4 ? 3 : 2) void attn_few_kernel(AttnFew a)
 {
-    constexpr int LANES = 4 * DT, SLOTS = 64 / LANES, U = kFewGroups<KIND>, TILE = 4 * U * SLOTS, DP = 32 * DT;
+    constexpr int LANES = 4 * DT, SLOTS = 64 / LANES, U = kFewGroups<R, KIND>, TILE = 4 * U * SLOTS, DP = 32 * DT;
     constexpr bool CODES = KIND != kFewFloat;
     __shared__ alignas(16) float outs[4 * SLOTS][R][DP];
     __shared__ float tops[4 * SLOTS][R], sums[4 * SLOTS][R];
@@ -246,7 +247,7 @@ void launch_few(const AttnFew &a, fmt_format_t f, dim3 grid, hipStream_t stream)
 
 }  // namespace
 
-int attention_few_tile(int dim, int32_t store) { return 4 * (store == FMT_STORE_CODE16 ? 4 : 2) * (dim <= 64 ? 8 : 4); }
+int attention_few_tile(int rows, int dim, int32_t store) { return 4 * (store == FMT_STORE_CODE16 && rows <= 2 ? 4 : 2) * (dim <= 64 ? 8 : 4); }
 
 int launch_attention_few(const AttnShape &s, const AttnView &q, const AttnView &k, const AttnView &v, const AttnView &o, float *lse, int32_t store,
                          int32_t result, int32_t splits, float *part, const ElemFormat &f, fmt_format_t fmt, hipStream_t stream)

@@ -10,44 +10,101 @@ extern template void run_attention_fwd<4>(const AttnFwd &, const FwdChoice &, di
 
 namespace {
 
-// Joins the parts of a row, a workgroup per row: each of its four waves takes every fourth part, a lane two columns.
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnFwd a)
+// Joins the parts of a row where they are few: a thread takes four columns, and reads all parts' lse and columns at once (a wave per row,
+// which waited for one after the other, took 10 us for 14000 rows).
+constexpr int kJoinFew = 8;
+__global__ __launch_bounds__(256) void attn_join_few_kernel(AttnFwd a)
 {
-    __shared__ float outs[4][128], sums[4], tops[4];
     const AttnShape &s = a.s;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len, at = blockIdx.x;
+    const int fours = (s.dim + 3) / 4;
+    const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len, n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (n >= all_rows * fours) return;
+    const int64_t at = n / fours;
+    const int col = static_cast<int>(n % fours) * 4, count = min(s.dim - col, 4);
     const float *lse = a.part + a.splits * all_rows * s.dim + at;
-    float top = -INFINITY;
-    for (int n = threadIdx.x; n < a.splits; n += 256) top = fmaxf(top, lse[n * all_rows]);
+    float l[kJoinFew], o[kJoinFew][4], top = -INFINITY, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-    if (lane == 0) tops[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    for (int i = 0; i < kJoinFew; ++i) {
+        const bool there = i < a.splits;
+        l[i] = there ? lse[i * all_rows] : -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[i][j] = there && j < count ? a.part[(i * all_rows + at) * s.dim + col + j] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < kJoinFew; ++i) top = fmaxf(top, l[i]);
     const float base = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, o[2] = {0.0f, 0.0f};
-#pragma unroll 4
-    for (int n = wave; n < a.splits; n += 4) {
-        const float w = exp2_fast(lse[n * all_rows] - base);
-        const float *part = a.part + (n * all_rows + at) * s.dim;
+#pragma unroll
+    for (int i = 0; i < kJoinFew; ++i) {
+        const float w = exp2_fast(l[i] - base);
         sum += w;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            if (lane + 64 * j < s.dim) o[j] = fmaf(w, part[lane + 64 * j], o[j]);
+        for (int j = 0; j < 4; ++j) v[j] = fmaf(w, o[i][j], v[j]);
     }
-    if (lane == 0) sums[wave] = sum;
-    outs[wave][lane] = o[0];
-    outs[wave][lane + 64] = o[1];
-    __syncthreads();
-    const int c = threadIdx.x;
-    if (c >= s.dim) return;
-    sum = sums[0] + sums[1] + sums[2] + sums[3];
-    const float out = sum == 0.0f ? 0.0f : (outs[0][c] + outs[1][c] + outs[2][c] + outs[3][c]) / sum;
+    const float over = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] *= over;
     const int t = static_cast<int>(at % s.q_len), head = static_cast<int>(at / s.q_len % s.heads), b = static_cast<int>(at / s.q_len / s.heads);
-    const float v[4] = {out, 0.0f, 0.0f, 0.0f};
+    store4(const_cast<void *>(a.o.p), b * a.o.sb + t * a.o.st + head * a.o.sh + col, count, v, a.result, a.f);
+    if (col == 0 && a.lse) a.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
+// And where they are many, a workgroup per row: first all parts' weights, then 8 or 16 threads per column with 8 parts each on their way.
+constexpr int kJoinMost = 2048, kJoinThreads = 1024, kJoinWaves = kJoinThreads / 64;
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnFwd a)
+{
+    __shared__ float weights[kJoinMost], outs[kJoinThreads], tops[kJoinWaves], sums[kJoinWaves];
+    const AttnShape &s = a.s;
+    const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len, at = blockIdx.x;
+    const float *lse = a.part + a.splits * all_rows * s.dim + at;
+    float top = -INFINITY, sum = 0.0f;
+    for (int n = threadIdx.x; n < a.splits; n += kJoinThreads) top = fmaxf(top, weights[n] = lse[n * all_rows]);
+#pragma unroll
+    for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinWaves; ++w) top = fmaxf(top, tops[w]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    for (int n = threadIdx.x; n < a.splits; n += kJoinThreads) sum += weights[n] = exp2_fast(weights[n] - base);
+#pragma unroll
+    for (int w = 32; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinWaves; ++w) sum += sums[w];
+    const int width = s.dim <= 64 ? 64 : 128, groups = kJoinThreads / width, c = threadIdx.x % width, g = threadIdx.x / width;
+    float o = 0.0f;
+    if (c < s.dim) {
+        const float *part = a.part + at * s.dim + c;
+        for (int n0 = g; n0 < a.splits; n0 += 8 * groups) {
+            float p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = n0 + i * groups < a.splits ? part[(n0 + i * groups) * all_rows * s.dim] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o = fmaf(n0 + i * groups < a.splits ? weights[n0 + i * groups] : 0.0f, p[i], o);
+        }
+    }
+    outs[threadIdx.x] = o;
+    __syncthreads();
+    if (g != 0 || c >= s.dim) return;
+    for (int i = 1; i < groups; ++i) o += outs[c + i * width];
+    o = sum == 0.0f ? 0.0f : o / sum;
+    const int t = static_cast<int>(at % s.q_len), head = static_cast<int>(at / s.q_len % s.heads), b = static_cast<int>(at / s.q_len / s.heads);
+    const float v[4] = {o, 0.0f, 0.0f, 0.0f};
     store4(const_cast<void *>(a.o.p), b * a.o.sb + t * a.o.st + head * a.o.sh + c, 1, v, a.result, a.f);
     if (c == 0 && a.lse) a.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
+int launch_join(const AttnFwd &a, hipStream_t stream)
+{
+    const int64_t all_rows = static_cast<int64_t>(a.s.batch) * a.s.heads * a.s.q_len, fours = (a.s.dim + 3) / 4;
+    if (a.splits > 1 && a.splits <= kJoinFew)
+        attn_join_few_kernel<<<dim3(static_cast<uint32_t>((all_rows * fours + 255) / 256)), dim3(256), 0, stream>>>(a);
+    else if (a.splits > 1)
+        attn_join_kernel<<<dim3(static_cast<uint32_t>(all_rows)), dim3(kJoinThreads), 0, stream>>>(a);
+    FMT_HIP_CHECK(hipGetLastError());
+    return FMT_OK;
 }
 
 }  // namespace
@@ -60,11 +117,12 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
     if (rc != FMT_OK) return rc;
     const bool few = static_cast<int64_t>(s.q_len) * s.group <= kFewRows;
     const int64_t row_tiles = few ? 1 : (static_cast<int64_t>(s.q_len) * s.group + kFwdRows - 1) / kFwdRows;
-    // few rows, long keys: their keys in parts of four tiles or more, until the compute units have a workgroup each (four of the kernel for
-    // few rows, whose workgroups wait for memory)
-    const int64_t work = row_tiles * s.kv_heads * s.batch, tile = few ? attention_few_tile(s.dim, store) : kFwdKeys, key_tiles = (s.k_len + tile - 1) / tile;
-    const int64_t want = few ? 4 * cus : cus;
-    int64_t splits = work >= want ? 1 : (want + work - 1) / work;
+    // few rows, long keys: their keys in parts of four tiles or more, until the compute units have a workgroup each, or in the kernel for
+    // few rows, which waits for memory, as many as they hold at a time (one more would be a second round for all of them)
+    const int64_t work = row_tiles * s.kv_heads * s.batch, tile = few ? attention_few_tile(s.q_len * s.group, s.dim, store) : kFwdKeys, key_tiles = (s.k_len + tile - 1) / tile;
+    const int64_t held = static_cast<int64_t>(cus) * (s.q_len * s.group <= 1 ? 4 : s.q_len * s.group <= 4 ? 3 : 2);
+    int64_t splits = few ? held / work : (cus + work - 1) / work;
+    if (splits > kJoinMost) splits = kJoinMost;
     if (splits > key_tiles / 4) splits = key_tiles / 4;
     if (splits < 1) splits = 1;
     const bool half = attention_half(fmt), check = fmt.e > 5;
@@ -78,18 +136,13 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
     }
     if (few) {
         rc = launch_attention_few(s, q, k, v, o, lse, store, result, a.splits, a.part, f, fmt, stream);
-        if (rc != FMT_OK) return rc;
-        if (splits > 1) attn_join_kernel<<<dim3(static_cast<uint32_t>(all_rows)), dim3(256), 0, stream>>>(a);
-        FMT_HIP_CHECK(hipGetLastError());
-        return FMT_OK;
+        return rc != FMT_OK ? rc : launch_join(a, stream);
     }
     const FwdChoice choice{half, half_pieces(fmt, result) == 2, a.codes, check};
     const dim3 blocks(static_cast<uint32_t>(grid));
     if (s.dim <= 64) run_attention_fwd<2>(a, choice, blocks, stream);
     else run_attention_fwd<4>(a, choice, blocks, stream);
-    if (splits > 1) attn_join_kernel<<<dim3(static_cast<uint32_t>(all_rows)), dim3(256), 0, stream>>>(a);
-    FMT_HIP_CHECK(hipGetLastError());
-    return FMT_OK;
+    return launch_join(a, stream);
 }
 
 }  // namespace fmt

@@ -214,7 +214,7 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
                          int32_t store, int32_t result, const ElemFormat &f, fmt_format_t fmt, hipStream_t stream);
 // At most kFewRows rows per (batch, kv head): splits parts of a sequence's keys, whose outputs go to `part` where there are several.
 constexpr int kFewRows = 8;
-int attention_few_tile(int dim, int32_t store);
+int attention_few_tile(int rows, int dim, int32_t store);
 int launch_attention_few(const AttnShape &s, const AttnView &q, const AttnView &k, const AttnView &v, const AttnView &o, float *lse, int32_t store,
                          int32_t result, int32_t splits, float *part, const ElemFormat &f, fmt_format_t fmt, hipStream_t stream);
 int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &k, const AttnView &v, const AttnView &o, const AttnView &go,

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfmt.so")
 SOURCES = ["fmt_api.hip", "fmt_stream.hip", "fmt_gemm.hip", "fmt_product_0.hip", "fmt_product_1.hip", "fmt_product_2.hip",
            "fmt_product_3.hip", "fmt_product_window.hip", "fmt_direct.hip", "fmt_fmac8.hip", "fmt_linear.hip", "fmt_dls.hip",
-           "fmt_norm.hip", "fmt_attention_fwd.hip", "fmt_attention_fwd_64.hip", "fmt_attention_fwd_128.hip", "fmt_attention_few.hip", "fmt_attention_bwd.hip",
+           "fmt_dropout.hip", "fmt_norm_fwd.hip", "fmt_norm_bwd.hip", "fmt_attention_fwd.hip", "fmt_attention_fwd_64.hip", "fmt_attention_fwd_128.hip", "fmt_attention_few.hip", "fmt_attention_bwd.hip",
            "fmt_attention_bwd_64.hip", "fmt_attention_bwd_128.hip"]
 # packed-fp32 instructions (v_pk_add_f32 and friends) are kept out of the generated code on purpose:
 # the rounding relies on every fp32 addition being one correctly rounded scalar operation

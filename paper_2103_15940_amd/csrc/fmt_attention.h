@@ -31,7 +31,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct AttnSeq {              // one sequence's length and the position of its first query
     int length, first;
@@ -260,42 +259,6 @@ __device__ __forceinline__ void f16_pieces(const float (&v)[8], u32x4 (&out)[N])
     }
 }
 
-typedef uint32_t u32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
-
-// Eight elements as they lie in memory.
-template <bool CODES>
-struct RawEight {
-    u32x4 w[CODES ? 1 : 2];
-};
-
-template <bool CODES>
-__device__ __forceinline__ RawEight<CODES> raw_load(const void *x, int64_t at, int count)
-{
-    RawEight<CODES> r;
-    typedef std::conditional_t<CODES, u32x4_any2, u32x4_any4> u32x4_any;
-#pragma unroll
-    for (int n = 0; n < (CODES ? 1 : 2); ++n) r.w[n] = u32x4{0u, 0u, 0u, 0u};
-    if (count >= 8) {
-        const u32x4_any *s = reinterpret_cast<const u32x4_any *>(static_cast<const char *>(x) + at * (CODES ? 2 : 4));
-#pragma unroll
-        for (int n = 0; n < (CODES ? 1 : 2); ++n) r.w[n] = s[n];
-    } else if (count > 0) {
-        if constexpr (CODES) {
-            const uint16_t *s = static_cast<const uint16_t *>(x) + at;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < count) r.w[0][i / 2] |= static_cast<uint32_t>(s[i]) << (16 * (i & 1));
-        } else {
-            const uint32_t *s = static_cast<const uint32_t *>(x) + at;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < count) r.w[i / 4][i % 4] = s[i];
-        }
-    }
-    return r;
-}
-
 // Their values in fp32, rounded to the format.
 template <bool CODES>
 __device__ __forceinline__ void raw_values(const RawEight<CODES> &r, float (&v)[8], const ElemFormat &f)
@@ -501,7 +464,9 @@ __device__ __forceinline__ void store_row(void *y, int64_t base, int half, int d
             uint16_t c[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint16_t h = __builtin_bit_cast(uint16_t, static_cast<_Float16>(v[i]));
+                float x = v[i];
+                asm("" : "+v"(x));                 // (see round_kind)
+                const uint16_t h = __builtin_bit_cast(uint16_t, static_cast<_Float16>(x));
                 c[i] = v[i] != v[i] ? static_cast<uint16_t>(0x7E00u) : h;
             }
             codes(col, count, c);

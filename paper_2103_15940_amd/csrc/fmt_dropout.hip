@@ -1,0 +1,58 @@
+// Dropout of a matrix (fmt_norm.h has the mathematics).  Bound by memory, and not far from the vector units' time for the generator.
+#include "fmt_norm.h"
+
+namespace fmt {
+
+namespace {
+
+constexpr int kDropThreads = 256, kDropRuns = 4;      // eights per thread
+
+template <int KIND, bool CODES, bool OUT>
+__global__ __launch_bounds__(kDropThreads) void dropout_kernel(const void *x, int64_t ldx, void *y, int64_t ldy, int64_t rows,
+                                                                int64_t cols, uint32_t blocks, Drop d, bool round, ElemFormat f)
+{
+    const uint64_t total = static_cast<uint64_t>(rows) * blocks, first = static_cast<uint64_t>(blockIdx.x) * (kDropThreads * kDropRuns);
+    const uint64_t row0 = first / blocks;
+    const uint32_t at0 = static_cast<uint32_t>(first - row0 * blocks);
+    RawEight<CODES> raw[kDropRuns];
+    int64_t to[kDropRuns];
+    int count[kDropRuns];
+#pragma unroll
+    for (int i = 0; i < kDropRuns; ++i) {
+        const uint32_t step = threadIdx.x + kDropThreads * i, past = at0 + step, over = past / blocks, g = past - over * blocks;
+        const int64_t row = static_cast<int64_t>(row0 + over), col = static_cast<int64_t>(g) * 8;
+        count[i] = first + step < total ? static_cast<int>(cols - col < 8 ? cols - col : 8) : 0;
+        to[i] = row * ldy + col;
+        raw[i] = raw_load<CODES>(x, row * ldx + col, count[i]);
+    }
+    const DropKey key = drop_key(d);
+#pragma unroll
+    for (int i = 0; i < kDropRuns; ++i) {
+        if (count[i] <= 0) break;
+        float v[8];
+        kind_values<KIND, CODES>(raw[i], v, f);
+        drop8(v, first + threadIdx.x + kDropThreads * i, key, d);
+        kind_store<KIND, OUT>(y, to[i], count[i], v, round, f);
+    }
+}
+
+}  // namespace
+
+int launch_dropout(const void *x, int64_t ldx, void *y, int64_t ldy, int64_t rows, int64_t cols, const fmt_dropout_t &d, int32_t store,
+                   int32_t result, const ElemFormat &f, hipStream_t stream)
+{
+    Drop drop = make_drop(d);
+    drop.rng = d.rng;
+    const uint32_t blocks = static_cast<uint32_t>((cols + 7) / 8);
+    const uint64_t grid = (static_cast<uint64_t>(rows) * blocks + kDropThreads * kDropRuns - 1) / (kDropThreads * kDropRuns);
+    if (grid > 0x7FFFFFFFull) return FMT_ERR_SHAPE;
+    with_kind(f, store, result, [&](auto kind, auto in, auto out) {
+        dropout_kernel<decltype(kind)::value, decltype(in)::value, decltype(out)::value>
+            <<<dim3(static_cast<uint32_t>(grid)), dim3(kDropThreads), 0, stream>>>(x, ldx, y, ldy, rows, cols, blocks, drop,
+                                                                                   result != FMT_RESULT_F32, f);
+    });
+    FMT_HIP_CHECK(hipGetLastError());
+    return FMT_OK;
+}
+
+}  // namespace fmt

@@ -2,6 +2,8 @@
 // the format's own 16-bit codes; and results as unrounded fp32, rounded fp32 or codes.
 #pragma once
 
+#include <type_traits>
+
 #include "fmt_quant.h"
 
 namespace fmt {
@@ -22,7 +24,10 @@ __device__ __forceinline__ void round_values(float (&v)[N], const ElemFormat &f)
     if (f.codec == kCodecNone) return;
     if (f.codec == kCodecHalf) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = static_cast<float>(static_cast<_Float16>(v[i]));
+        for (int i = 0; i < N; ++i) {
+            asm("" : "+v"(v[i]));              // (see round_kind)
+            v[i] = static_cast<float>(static_cast<_Float16>(v[i]));
+        }
         return;
     }
     if (p.mode == kModeInteger) {
@@ -144,6 +149,182 @@ __device__ __forceinline__ void load8_any(const void *x, int64_t at, int count, 
 {
     if (codes) load8<true>(x, at, count, v, f);
     else load8<false>(x, at, count, v, f);
+}
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_any2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_any4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// Eight elements as they lie in memory.
+template <bool CODES>
+struct RawEight {
+    u32x4 w[CODES ? 1 : 2];
+};
+
+template <bool CODES>
+__device__ __forceinline__ RawEight<CODES> raw_load(const void *x, int64_t at, int count)
+{
+    RawEight<CODES> r;
+    typedef std::conditional_t<CODES, u32x4_any2, u32x4_any4> u32x4_any;
+#pragma unroll
+    for (int n = 0; n < (CODES ? 1 : 2); ++n) r.w[n] = u32x4{0u, 0u, 0u, 0u};
+    if (count >= 8) {
+        const u32x4_any *s = reinterpret_cast<const u32x4_any *>(static_cast<const char *>(x) + at * (CODES ? 2 : 4));
+#pragma unroll
+        for (int n = 0; n < (CODES ? 1 : 2); ++n) r.w[n] = s[n];
+    } else if (count > 0) {
+        if constexpr (CODES) {
+            const uint16_t *s = static_cast<const uint16_t *>(x) + at;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) r.w[0][i / 2] |= static_cast<uint32_t>(s[i]) << (16 * (i & 1));
+        } else {
+            const uint32_t *s = static_cast<const uint32_t *>(x) + at;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) r.w[i / 4][i % 4] = s[i];
+        }
+    }
+    return r;
+}
+
+// ---- the same with the way of rounding known at compile time, for kernels that are bound by memory: the paths of other formats would
+// lie between their loads and cost them misses of the instruction cache
+
+enum : int {
+    kKindNone = 0,     // 1/8/23 with denormals
+    kKindHalf = 1,     // 1/5/10 with denormals
+    kKindMagic = 2,    // e < 8, m <= 22
+    kKindInteger = 3,  // e == 8
+    kKindMixed = 4     // e < 8, m == 23
+};
+
+inline int elem_kind(const ElemFormat &f)
+{
+    if (f.codec == kCodecNone) return kKindNone;
+    if (f.codec == kCodecHalf) return kKindHalf;
+    return f.p.mode == kModeMagic ? kKindMagic : f.p.mode == kModeInteger ? kKindInteger : kKindMixed;
+}
+
+template <int KIND>
+__device__ __forceinline__ void round_kind(float (&v)[8], const ElemFormat &f)
+{
+    if constexpr (KIND == kKindNone) return;
+    const uint32_t flush = f.ftz ? f.p.t_den : 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t u = __float_as_uint(v[i]);
+        if constexpr (KIND == kKindHalf) {
+            // the fp32 value itself is what is rounded: product and conversion in one instruction would round once, and lose the sign of -0
+            asm("" : "+v"(v[i]));
+            v[i] = static_cast<float>(static_cast<_Float16>(v[i]));
+        } else {
+            constexpr int kMode = KIND == kKindMagic ? kModeMagic : KIND == kKindInteger ? kModeInteger : kModeMixed;
+            const uint32_t r = quantize_bits<kMode, false>(u, f.p);
+            v[i] = __uint_as_float((u & 0x7FFFFFFFu) < flush ? u & 0x80000000u : r);
+        }
+    }
+}
+
+template <int KIND>
+__device__ __forceinline__ void decode_kind(const u32x4 &w, float (&v)[8], const ElemFormat &f)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t c = w[i / 2] >> (16 * (i & 1)) & 0xFFFFu;
+        if constexpr (KIND == kKindHalf) v[i] = static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(c)));
+        else if constexpr (KIND == kKindInteger) v[i] = __uint_as_float(c << (31u - f.p.sign_pos));     // the code is the pattern's upper part
+        else v[i] = __uint_as_float(decode_bits<false>(c, f.p));
+    }
+}
+
+// Values of the format to codes.
+template <int KIND>
+__device__ __forceinline__ u32x4 encode_kind(const float (&v)[8], const ElemFormat &f)
+{
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        uint32_t c[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float x = v[i + j];
+            if constexpr (KIND == kKindHalf) {
+                const uint16_t h = __builtin_bit_cast(uint16_t, static_cast<_Float16>(x));
+                c[j] = x != x ? 0x7E00u : h;
+            } else if constexpr (KIND == kKindInteger) {
+                c[j] = __float_as_uint(x) >> (31u - f.p.sign_pos);
+            } else {
+                c[j] = encode_bits<kModeMagic>(__float_as_uint(x), f.p);
+            }
+        }
+        w[i / 2] = c[0] | c[1] << 16;
+    }
+    return w;
+}
+
+// R of what raw_load gave.
+template <int KIND, bool CODES>
+__device__ __forceinline__ void kind_values(const RawEight<CODES> &r, float (&v)[8], const ElemFormat &f)
+{
+    if constexpr (CODES) {
+        decode_kind<KIND>(r.w[0], v, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i / 4][i % 4]);
+        round_kind<KIND>(v, f);
+    }
+}
+
+// The first `count` of eight results to y[at]: codes, or fp32 that is rounded or not (`round`, uniform).  ROUNDED: the values are the format's.
+template <int KIND, bool CODES, bool ROUNDED = false>
+__device__ __forceinline__ void kind_store(void *y, int64_t at, int count, float (&v)[8], bool round, const ElemFormat &f)
+{
+    if constexpr (!ROUNDED) {
+        if (CODES || round) round_kind<KIND>(v, f);
+    }
+    if constexpr (CODES) {
+        const u32x4 w = encode_kind<KIND>(v, f);
+        uint16_t *d = static_cast<uint16_t *>(y) + at;
+        if (count >= 8) {
+            *reinterpret_cast<u32x4_any2 *>(d) = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) d[i] = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));
+        }
+    } else {
+        float *d = static_cast<float *>(y) + at;
+        if (count >= 8) {
+            *reinterpret_cast<f32x4_any *>(d) = f32x4_any{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4_any *>(d + 4) = f32x4_any{v[4], v[5], v[6], v[7]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < count) d[i] = v[i];
+        }
+    }
+}
+
+// run(KIND, codes in, codes out) for a format and the tensors' types; formats without 16-bit codes have no codes.
+template <class RUN>
+void with_kind(const ElemFormat &f, int32_t store, int32_t result, RUN &&run)
+{
+    using std::integral_constant;
+    const bool in = store == FMT_STORE_CODE16, out = result == FMT_RESULT_CODE16;
+    auto types = [&](auto kind) {
+        if (in && out) run(kind, std::true_type{}, std::true_type{});
+        else if (in) run(kind, std::true_type{}, std::false_type{});
+        else if (out) run(kind, std::false_type{}, std::true_type{});
+        else run(kind, std::false_type{}, std::false_type{});
+    };
+    switch (elem_kind(f)) {
+    case kKindNone: run(integral_constant<int, kKindNone>{}, std::false_type{}, std::false_type{}); break;
+    case kKindMixed: run(integral_constant<int, kKindMixed>{}, std::false_type{}, std::false_type{}); break;
+    case kKindHalf: types(integral_constant<int, kKindHalf>{}); break;
+    case kKindMagic: types(integral_constant<int, kKindMagic>{}); break;
+    default: types(integral_constant<int, kKindInteger>{}); break;
+    }
 }
 
 }  // namespace fmt

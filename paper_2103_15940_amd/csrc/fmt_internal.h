@@ -180,7 +180,7 @@ inline ElemFormat make_elem_format(fmt_format_t f, const QuantParams &p)
     return ElemFormat{p, f.denorm == 0, codec};
 }
 
-// Row-wise operators (fmt_norm.hip).
+// Row-wise operators (fmt_dropout.hip, fmt_norm_fwd.hip, fmt_norm_bwd.hip).
 struct LayerNorm {
     int64_t rows, cols;
     fmt_dropout_t drop;

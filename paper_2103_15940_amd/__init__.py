@@ -753,7 +753,7 @@ def dls_state_to_dict(state) -> dict:
 
 
 # Operators beside the products: tensors of fp32 values, or of 16-bit codes (int16 / uint16; float16 is the codes of 1/5/10 and
-# bfloat16 those of 1/8/7).
+# bfloat16 those of 1/8/7).  Small calls are bound by the host, so the common case of every check comes first and is one expression.
 _RESULTS = {"f32": 0, "round": 1, "code16": 2}
 _CODE_FORMATS = {torch.float16: (5, 10), torch.bfloat16: (8, 7)}
 
@@ -762,20 +762,21 @@ def _elem_store(t, name: str, fmt) -> int:
     """FMT_STORE_* of a tensor's type."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a tensor on the GPU" % name)
-    if t.dtype == torch.float32:
+    dtype = t.dtype
+    if dtype is torch.float32:
         return 0
-    if t.dtype in (torch.int16, torch.uint16):
+    if dtype in (torch.int16, torch.uint16):
         return 1
-    if t.dtype in _CODE_FORMATS:
-        if _CODE_FORMATS[t.dtype] != (int(fmt[0]), int(fmt[1])):
-            raise TypeError("%s is %s, which holds codes of 1/%d/%d, not of 1/%d/%d" % (name, t.dtype, *_CODE_FORMATS[t.dtype], fmt[0], fmt[1]))
+    if dtype in _CODE_FORMATS:
+        if _CODE_FORMATS[dtype] != (int(fmt[0]), int(fmt[1])):
+            raise TypeError("%s is %s, which holds codes of 1/%d/%d, not of 1/%d/%d" % (name, dtype, *_CODE_FORMATS[dtype], fmt[0], fmt[1]))
         return 1
     raise TypeError("%s must be float32, or int16, uint16, float16 or bfloat16 codes" % name)
 
 
 def _elem_result(result, like):
     """FMT_RESULT_* and the type of the tensors that are written; by default they are stored as the inputs are, rounded."""
-    code = like.dtype != torch.float32
+    code = like.dtype is not torch.float32
     if result is None:
         result = "code16" if code else "round"
     if result not in _RESULTS:
@@ -784,29 +785,44 @@ def _elem_result(result, like):
 
 
 def _same_kind(t, like, name: str):
-    if not isinstance(t, torch.Tensor) or t.dtype != like.dtype or t.shape != like.shape or t.device != like.device:
+    if not isinstance(t, torch.Tensor) or t.dtype is not like.dtype or t.shape != like.shape or t.device != like.device:
         raise TypeError("%s must have the type, shape and device of the first tensor" % name)
     return t
 
 
 def _as_rows(t, name: str):
-    """(tensor of rows x last dimension, leading dimension), without a copy."""
-    if t.dim() < 1:
+    """(pointer, rows, columns, leading dimension) of a tensor as a matrix of its last dimension, without a copy."""
+    shape = t.shape
+    if len(shape) == 2:
+        rows, cols = shape
+        ld, unit = t.stride()
+    elif len(shape) == 1:
+        rows, cols, ld, unit = 1, shape[0], shape[0], t.stride(0)
+    elif not shape:
         raise ValueError("%s must have at least one dimension" % name)
-    cols = t.shape[-1]
-    r = t if t.dim() == 2 else t.reshape(1, cols) if t.dim() == 1 else t.view(-1, cols) if t.numel() else t.reshape(0, max(cols, 1))
-    if r.shape[1] > 1 and r.stride(1) != 1:
+    else:
+        cols = shape[-1]
+        if t.is_contiguous():
+            rows, ld, unit = (t.numel() // cols if cols else 0), cols, 1
+        else:
+            r = t.view(-1, cols)
+            rows, (ld, unit) = r.shape[0], r.stride()
+    if unit != 1 and cols > 1:
         raise ValueError("%s must have unit stride along its last dimension" % name)
-    return r, (r.stride(0) if r.shape[0] > 1 else max(r.shape[1], 1))
+    return t.data_ptr(), rows, cols, (ld if rows > 1 else cols or 1)
 
 
 def _param(t, name: str, n: int, device):
     if t is None:
         return None
-    _dev_f32(t, name)
-    if t.numel() != n or not t.is_contiguous() or t.device != device:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.float32 or t.numel() != n or t.device != device or not t.is_contiguous():
         raise ValueError("%s must be a contiguous float32 tensor of %d values on the inputs' device" % (name, n))
     return t.data_ptr()
+
+
+def _new_like(t, dtype):
+    """An uninitialised contiguous tensor of t's shape."""
+    return torch.empty_like(t) if t.dtype is dtype and t.is_contiguous() else t.new_empty(t.shape, dtype=dtype)
 
 
 def new_rng(seed: int, step: int = 0, device="cuda"):
@@ -817,12 +833,12 @@ def new_rng(seed: int, step: int = 0, device="cuda"):
 
 
 def _dropout_arg(p, site, rng, device) -> _CDropout:
-    if rng is not None and (not isinstance(rng, torch.Tensor) or rng.dtype != torch.int64 or rng.numel() != 2 or not rng.is_contiguous()
+    if rng is not None and (not isinstance(rng, torch.Tensor) or rng.dtype is not torch.int64 or rng.numel() != 2 or not rng.is_contiguous()
                             or rng.device != device):
         raise TypeError("rng must be a contiguous int64 tensor of two values on the inputs' device (see new_rng)")
-    if not 0 <= int(site) < 1 << 32:
+    if not 0 <= site < 1 << 32:
         raise ValueError("site must be in [0, 2^32)")
-    return _CDropout(float(p), int(site), None if rng is None else rng.data_ptr())
+    return _CDropout(p, site, None if rng is None else rng.data_ptr())
 
 
 def fmt_dropout(x, p: float, rng, fmt, site: int = 0, result=None, out=None, stream=None):
@@ -830,17 +846,19 @@ def fmt_dropout(x, p: float, rng, fmt, site: int = 0, result=None, out=None, str
     x: float32, rounded to the format as it is read, or 16-bit codes.  ``result``: 'f32' (unrounded), 'round' or 'code16';
     by default as x is stored, rounded."""
     store = _elem_store(x, "x", fmt)
-    rows, ldx = _as_rows(x, "x")
+    xp, rows, cols, ldx = _as_rows(x, "x")
     res, dtype = _elem_result(result, x)
     d = _dropout_arg(p, site, rng, x.device)
     if out is None:
-        out = torch.empty(x.shape, dtype=dtype, device=x.device)
-    if out.dtype != dtype or out.shape != x.shape or out.device != x.device:
-        raise ValueError("out must be a tensor of x's shape and of the type of the result")
-    orows, ldy = _as_rows(out, "out")
-    rc = _lib.fmt_dropout(rows.data_ptr(), ldx, orows.data_ptr(), ldy, rows.shape[0], rows.shape[1], d, store, res, _cfmt(fmt),
-                          _call_stream(stream))
-    _check(rc, "fmt_dropout")
+        out = _new_like(x, dtype)
+        yp, ldy = out.data_ptr(), cols or 1
+    else:
+        if out.dtype is not dtype or out.shape != x.shape or out.device != x.device:
+            raise ValueError("out must be a tensor of x's shape and of the type of the result")
+        yp, _, _, ldy = _as_rows(out, "out")
+    rc = _lib.fmt_dropout(xp, ldx, yp, ldy, rows, cols, d, store, res, _cfmt(fmt), _call_stream(stream))
+    if rc:
+        raise FmtError(rc, "fmt_dropout")
     return out
 
 
@@ -850,22 +868,26 @@ def fmt_layernorm_fwd(x, gamma, beta, fmt, residual=None, p: float = 0.0, rng=No
     (y, z, mean, rstd); z is None where it is R(x): the backward pass then takes x.  ``keep=False`` (inference): z, mean and
     rstd are not written and come back as None.  x, residual: float32 or 16-bit codes; gamma, beta: float32, or None."""
     store = _elem_store(x, "x", fmt)
-    rows, ldx = _as_rows(x, "x")
-    n, cols = rows.shape
+    xp, n, cols, ldx = _as_rows(x, "x")
+    device = x.device
     res, dtype = _elem_result(result, x)
     rp, ldr = None, 0
     if residual is not None:
-        rr, ldr = _as_rows(_same_kind(residual, x, "residual"), "residual")
-        rp = rr.data_ptr()
-    d = _dropout_arg(p, site, rng, x.device)
-    y = torch.empty(x.shape, dtype=dtype, device=x.device)
-    z = torch.empty_like(y) if keep and (residual is not None or p > 0) else None
-    mean, rstd = torch.empty((2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device) if keep else (None, None)
-    rc = _lib.fmt_layernorm_fwd(n, cols, rows.data_ptr(), ldx, rp, ldr, d, _param(gamma, "gamma", cols, x.device),
-                                _param(beta, "beta", cols, x.device), float(eps), None if z is None else z.data_ptr(), cols, y.data_ptr(),
-                                cols, None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), store, res,
-                                _cfmt(fmt), _call_stream(stream))
-    _check(rc, "fmt_layernorm_fwd")
+        rp, _, _, ldr = _as_rows(_same_kind(residual, x, "residual"), "residual")
+    d = _dropout_arg(p, site, rng, device)
+    y = _new_like(x, dtype)
+    z = mean = rstd = zp = mp = sp = None
+    if keep:
+        if residual is not None or p > 0:
+            z = torch.empty_like(y)
+            zp = z.data_ptr()
+        mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
+        rstd = torch.empty_like(mean)
+        mp, sp = mean.data_ptr(), rstd.data_ptr()
+    rc = _lib.fmt_layernorm_fwd(n, cols, xp, ldx, rp, ldr, d, _param(gamma, "gamma", cols, device), _param(beta, "beta", cols, device), eps,
+                                zp, cols, y.data_ptr(), cols, mp, sp, store, res, _cfmt(fmt), _call_stream(stream))
+    if rc:
+        raise FmtError(rc, "fmt_layernorm_fwd")
     return y, z, mean, rstd
 
 
@@ -875,33 +897,38 @@ def fmt_layernorm_bwd(dy, z, mean, rstd, gamma, fmt, p: float = 0.0, rng=None, s
     same tensor as dz with p == 0).  ``z``: what the forward call returned, or its x where that was None; dy is stored
     as z is.  ``params=False``: dgamma and dbeta are not wanted."""
     store = _elem_store(dy, "dy", fmt)
-    _same_kind(z, dy, "z")
-    (rows, lddy), (zrows, ldz) = _as_rows(dy, "dy"), _as_rows(z, "z")
-    n, cols = rows.shape
+    dp, n, cols, lddy = _as_rows(dy, "dy")
+    zp, _, _, ldz = _as_rows(_same_kind(z, dy, "z"), "z")
+    device = dy.device
     res, dtype = _elem_result(result, dy)
-    d = _dropout_arg(p, site, rng, dy.device)
-    dz = torch.empty(dy.shape, dtype=dtype, device=dy.device)
+    d = _dropout_arg(p, site, rng, device)
+    dz = _new_like(dy, dtype)
     dx = torch.empty_like(dz) if p > 0 else None
-    dgamma, dbeta = torch.empty((2, cols), dtype=torch.float32, device=dy.device) if params else (None, None)
-    rc = _lib.fmt_layernorm_bwd(n, cols, rows.data_ptr(), lddy, zrows.data_ptr(), ldz, _param(mean, "mean", n, dy.device),
-                                _param(rstd, "rstd", n, dy.device), _param(gamma, "gamma", cols, dy.device), d, dz.data_ptr(), cols,
-                                None if dx is None else dx.data_ptr(), cols, None if dgamma is None else dgamma.data_ptr(),
-                                None if dbeta is None else dbeta.data_ptr(), store, res, _cfmt(fmt), _call_stream(stream))
-    _check(rc, "fmt_layernorm_bwd")
+    dgamma = dbeta = gp = bp = None
+    if params:
+        dgamma = dy.new_empty((cols,), dtype=torch.float32)
+        dbeta = torch.empty_like(dgamma)
+        gp, bp = dgamma.data_ptr(), dbeta.data_ptr()
+    rc = _lib.fmt_layernorm_bwd(n, cols, dp, lddy, zp, ldz, _param(mean, "mean", n, device), _param(rstd, "rstd", n, device),
+                                _param(gamma, "gamma", cols, device), d, dz.data_ptr(), cols, None if dx is None else dx.data_ptr(), cols,
+                                gp, bp, store, res, _cfmt(fmt), _call_stream(stream))
+    if rc:
+        raise FmtError(rc, "fmt_layernorm_bwd")
     return dz, (dz if dx is None else dx), dgamma, dbeta
 
 
 def _view4(t, name: str) -> _CView:
     """[batch, token, head, dim] with unit stride along dim."""
-    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+    strides = t.stride()
+    if len(strides) != 4 or (strides[3] != 1 and t.shape[3] > 1):
         raise ValueError("%s must be [batch, token, head, dim] with unit stride along dim" % name)
-    return _CView(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    return _CView(t.data_ptr(), strides[0], strides[1], strides[2])
 
 
 def _per_sequence(t, name: str, batch: int, device):
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.numel() != batch or not t.is_contiguous() or t.device != device:
+    if not isinstance(t, torch.Tensor) or t.dtype is not torch.int32 or t.numel() != batch or not t.is_contiguous() or t.device != device:
         raise TypeError("%s must be a contiguous int32 tensor with one value per sequence, on the inputs' device" % name)
     return t.data_ptr()
 
@@ -911,15 +938,16 @@ def _attention_args(q, k, v, fmt, causal, window, sinks, scale, k_lens, q_pos):
     store = _elem_store(q, "q", fmt)
     views = _view4(q, "q"), _view4(k, "k"), _view4(v, "v")
     b, nq, h, d = q.shape
-    if k.dtype != q.dtype or v.dtype != q.dtype or k.device != q.device or v.device != q.device:
+    kb, nk, hk, kd = k.shape
+    device = q.device
+    if k.dtype is not q.dtype or v.dtype is not q.dtype or k.device != device or v.device != device:
         raise TypeError("k and v must have the type and device of q")
-    if k.shape != v.shape or k.shape[0] != b or k.shape[3] != d:
+    if kb != b or kd != d or v.shape != k.shape:
         raise ValueError("k and v must be [batch, tokens, kv heads, dim] with q's batch and dim")
-    if not (0 <= int(window) < 1 << 30 and 0 <= int(sinks) < 1 << 30):
+    if not (0 <= window < 1 << 30 and 0 <= sinks < 1 << 30):
         raise ValueError("window and sinks must be in [0, 2^30)")
-    a = _CAttention(b, h, k.shape[2], nq, k.shape[1], d, 1 if causal else 0, int(window), int(sinks),
-                    d ** -0.5 if scale is None else float(scale), _per_sequence(k_lens, "k_lens", b, q.device),
-                    _per_sequence(q_pos, "q_pos", b, q.device))
+    a = _CAttention(b, h, hk, nq, nk, d, 1 if causal else 0, window, sinks, (d ** -0.5 if d else 0.0) if scale is None else scale,
+                    _per_sequence(k_lens, "k_lens", b, device), _per_sequence(q_pos, "q_pos", b, device))
     return store, a, views
 
 
@@ -932,11 +960,12 @@ def fmt_attention_fwd(q, k, v, fmt, causal: bool = False, window: int = 0, sinks
     None."""
     store, a, views = _attention_args(q, k, v, fmt, causal, window, sinks, scale, k_lens, q_pos)
     res, dtype = _elem_result(result, q)
-    o = torch.empty(q.shape, dtype=dtype, device=q.device)
-    lse = torch.empty((a.batch, a.heads, a.q_len), dtype=torch.float32, device=q.device) if keep else None
+    o = _new_like(q, dtype)
+    lse = q.new_empty((a.batch, a.heads, a.q_len), dtype=torch.float32) if keep else None
     rc = _lib.fmt_attention_fwd(a, *views, _view4(o, "o"), None if lse is None else lse.data_ptr(), store, res, _cfmt(fmt),
                                 _call_stream(stream))
-    _check(rc, "fmt_attention_fwd")
+    if rc:
+        raise FmtError(rc, "fmt_attention_fwd")
     return o, lse
 
 
@@ -946,15 +975,16 @@ def fmt_attention_bwd(d_o, q, k, v, o, lse, fmt, causal: bool = False, window: i
     store, a, views = _attention_args(q, k, v, fmt, causal, window, sinks, scale, k_lens, q_pos)
     res, dtype = _elem_result(result, q)
     for t, name in ((d_o, "d_o"), (o, "o")):
-        if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != q.shape or t.device != q.device:
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != q.shape or t.device != q.device:
             raise TypeError("%s must have q's shape and the type of the result" % name)
-    if not isinstance(lse, torch.Tensor) or lse.dtype != torch.float32 or tuple(lse.shape) != (a.batch, a.heads, a.q_len) \
+    if not isinstance(lse, torch.Tensor) or lse.dtype is not torch.float32 or lse.shape != (a.batch, a.heads, a.q_len) \
             or not lse.is_contiguous() or lse.device != q.device:
         raise TypeError("lse must be what fmt_attention_fwd returned")
-    dq, dk, dv = (torch.empty(t.shape, dtype=dtype, device=q.device) for t in (q, k, v))
+    dq, dk, dv = _new_like(q, dtype), _new_like(k, dtype), _new_like(v, dtype)
     rc = _lib.fmt_attention_bwd(a, *views, _view4(o, "o"), _view4(d_o, "d_o"), lse.data_ptr(), _view4(dq, "dq"), _view4(dk, "dk"),
                                 _view4(dv, "dv"), store, res, _cfmt(fmt), _call_stream(stream))
-    _check(rc, "fmt_attention_bwd")
+    if rc:
+        raise FmtError(rc, "fmt_attention_bwd")
     return dq, dk, dv
 
 

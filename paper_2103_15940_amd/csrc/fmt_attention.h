@@ -296,26 +296,49 @@ struct HalfCodes {
     int32_t shift, sign_shift;              // shift < 0: by way of fp32
 };
 
-// As fp16 times `up` (1: the format's values are fp16's; nothing is checked).  high: of codes the largest magnitudes, of either half of a word;
-// otherwise as above.
-template <bool CODES>
-__device__ __forceinline__ u32x4 raw_half(const RawEight<CODES> &r, float up, const HalfCodes &hc, uint32_t &high, const ElemFormat &f)
+// How elements become fp16, known at compile time (elem_kind's ways of rounding, and codes by their format).
+enum : int {
+    kHalfCodes = 0,      // codes of 1/5/10: as they are
+    kHalfFloat = 1,      // fp32, 1/5/10 with denormals: converted
+    kBf16Codes = 2,      // codes of 1/8/7
+    kSixCodes = 3,       // codes with e == 6, two at a time
+    kOtherCodes = 4,     // by way of fp32
+    kMagicFloat = 5,     // fp32, e < 8
+    kIntegerFloat = 6    // fp32, e == 8
+};
+constexpr bool half_is_codes(int kind) { return kind == kHalfCodes || kind == kBf16Codes || kind == kSixCodes || kind == kOtherCodes; }
+constexpr bool half_has_limit(int kind) { return kind != kHalfCodes && kind != kHalfFloat; }      // e <= 5 otherwise is told at run time
+
+inline int half_kind(fmt_format_t f, int32_t store)
 {
-    if constexpr (CODES) {
-        if (f.codec == kCodecHalf) return r.w[0];
-        u16x2 top = __builtin_bit_cast(u16x2, high);
-        u32x4 out;
-        if (f.codec == kCodecBf16) {
+    if (store == FMT_STORE_CODE16) return f.e == 5 && f.m == 10 ? kHalfCodes : f.e == 8 && f.m == 7 ? kBf16Codes : f.e == 6 ? kSixCodes : kOtherCodes;
+    return f.e == 5 && f.m == 10 && f.denorm ? kHalfFloat : f.e == 8 ? kIntegerFloat : kMagicFloat;
+}
+
+// Eight elements as fp16 times `up`.  high: the largest magnitude so far; of codes, of either half of a word; of fp32 as a bit pattern, unrounded.
+template <int KIND>
+__device__ __forceinline__ u32x4 raw_half(const RawEight<half_is_codes(KIND)> &r, float up, const HalfCodes &hc, uint32_t &high, const ElemFormat &f)
+{
+    u32x4 out;
+    if constexpr (KIND == kHalfCodes) {
+        return r.w[0];
+    } else if constexpr (KIND == kHalfFloat) {
+        f16x8 h;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t w = r.w[0][i];
-                top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu));
-                out[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xFFFF0000u) * up));
-            }
-            high = __builtin_bit_cast(uint32_t, top);
-            return out;
+        for (int i = 0; i < 8; ++i) h[i] = static_cast<_Float16>(__uint_as_float(r.w[i / 4][i % 4]));
+        return __builtin_bit_cast(u32x4, h);
+    } else if constexpr (KIND == kBf16Codes) {
+        u16x2 top = __builtin_bit_cast(u16x2, high);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = r.w[0][i];
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu));
+            out[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xFFFF0000u) * up));
         }
-        u16x2 low = {0xFFFF, 0xFFFF};
+        high = __builtin_bit_cast(uint32_t, top);
+        return out;
+    } else if constexpr (KIND == kSixCodes || KIND == kOtherCodes) {
+        u16x2 top = __builtin_bit_cast(u16x2, high), low = {0xFFFF, 0xFFFF};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const u16x2 body = __builtin_bit_cast(u16x2, r.w[0][i] & hc.body);
@@ -323,53 +346,42 @@ __device__ __forceinline__ u32x4 raw_half(const RawEight<CODES> &r, float up, co
             low = __builtin_elementwise_min(low, body - static_cast<uint16_t>(1));
         }
         high = __builtin_bit_cast(uint32_t, top);
-        // a code other than 0 whose fp16 is no normal number (|x| < 2^-23) is rare: then all go by way of fp32
-        const uint16_t normal = static_cast<uint16_t>((8u << (10 - max(hc.shift, 0))) - 1u);
-        if (hc.shift >= 0 && !__any(low[0] < normal || low[1] < normal)) {
+        if constexpr (KIND == kSixCodes) {
+            // a code other than 0 whose fp16 is no normal number (|x| < 2^-23) is rare: then all go by way of fp32
+            const uint16_t normal = static_cast<uint16_t>((8u << (10 - hc.shift)) - 1u);
+            if (!__any(low[0] < normal || low[1] < normal)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const u16x2 body = __builtin_bit_cast(u16x2, r.w[0][i] & hc.body) << static_cast<uint16_t>(hc.shift);
-                const u16x2 h = __builtin_elementwise_sub_sat(body, u16x2{7 << 10, 7 << 10});
-                out[i] = __builtin_bit_cast(uint32_t, h) | (r.w[0][i] & hc.sign) << hc.sign_shift;
+                for (int i = 0; i < 4; ++i) {
+                    const u16x2 body = __builtin_bit_cast(u16x2, r.w[0][i] & hc.body) << static_cast<uint16_t>(hc.shift);
+                    const u16x2 h = __builtin_elementwise_sub_sat(body, u16x2{7 << 10, 7 << 10});
+                    out[i] = __builtin_bit_cast(uint32_t, h) | (r.w[0][i] & hc.sign) << hc.sign_shift;
+                }
+                return out;
             }
-            return out;
         }
-    }
-    if constexpr (!CODES) {
+        float v[8];
+        raw_values(r, v, f);
+        uint32_t ignore = 0;
+        return to_half(v, up, ignore);
+    } else {
         // the short roundings: what they do not serve is above the limit.  (Formats of more than 10 bits do not come here.)
         const QuantParams &p = f.p;
-        u32x4 out;
         const uint32_t flush = f.ftz ? p.t_den : 0u;
-        auto run = [&](auto round) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const uint32_t a = r.w[i / 4][i % 4], b = r.w[i / 4][i % 4 + 1];
-                high = max(max(a & 0x7FFFFFFFu, b & 0x7FFFFFFFu), high);
-                out[i / 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(round(a) * up, round(b) * up));
-            }
+        const RoundMasks k = round_masks(p);
+        auto round = [&](uint32_t u) __attribute__((always_inline)) {
+            uint32_t q;
+            if constexpr (KIND == kMagicFloat) q = quantize_short<kModeMagic, false, false>(u, p, k);
+            else q = (u + p.rbias + __builtin_amdgcn_ubfe(u, p.shift, p.lsb_width)) & p.nmask;
+            return __uint_as_float((u & 0x7FFFFFFFu) < flush ? 0u : q);
         };
-        if (f.codec == kCodecHalf) {
-            f16x8 h;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = static_cast<_Float16>(__uint_as_float(r.w[i / 4][i % 4]));
-            return __builtin_bit_cast(u32x4, h);
-        }
-        if (p.mode == kModeMagic) {
-            const RoundMasks k = round_masks(p);
-            if (f.ftz) run([&](uint32_t u) { return __uint_as_float((u & 0x7FFFFFFFu) < flush ? 0u : quantize_short<kModeMagic, false, false>(u, p, k)); });
-            else run([&](uint32_t u) { return __uint_as_float(quantize_short<kModeMagic, false, false>(u, p, k)); });
-        } else {
-            run([&](uint32_t u) {
-                const uint32_t q = (u + p.rbias + __builtin_amdgcn_ubfe(u, p.shift, p.lsb_width)) & p.nmask;
-                return __uint_as_float((u & 0x7FFFFFFFu) < flush ? 0u : q);
-            });
+        for (int i = 0; i < 8; i += 2) {
+            const uint32_t a = r.w[i / 4][i % 4], b = r.w[i / 4][i % 4 + 1];
+            high = max(max(a & 0x7FFFFFFFu, b & 0x7FFFFFFFu), high);
+            out[i / 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(round(a) * up, round(b) * up));
         }
         return out;
     }
-    float v[8];
-    raw_values(r, v, f);
-    uint32_t ignore = 0;
-    return to_half(v, up, ignore);
 }
 
 // R(Q) is multiplied by the scale's sign, so that scores are ordered as they come out of the product; a scale of 0 makes it 0.

@@ -17,12 +17,13 @@ struct AttnBwd {
     uint16_t *qh, *gh;        // fp16 operands: [batch][kv_heads][row_tiles * 128][32 DT] Q and dO, zero past the last row and column,
     uint16_t *kh, *vh;        // [batch][kv_heads][key_tiles * 128][32 DT] K and V, zero past the sequence's length
     uint32_t *highs;          // the largest |x| of each 32 rows of Q, then of each 32 keys of K, then of V
-    float *part;              // parts > 1: [2][parts][batch][k_len][kv_heads][dim] of dK, dV
+    float *part;              // [2][parts][batch][part_keys][kv_heads][dim] of dK, dV
     float up;                 // what the fp16 operands are multiplied by
     bool check;               // whether that has a limit
     bool codes, gcodes;       // how q, k and v, and o and go, are stored
-    int32_t parts;            // parts of the rows that a tile of keys adds up
-    uint32_t key_tiles, row_tiles, key_blocks, row_blocks;
+    int32_t parts;            // parts of the rows that each of the first part_tiles tiles of keys adds up
+    int32_t part_keys;        // their keys
+    uint32_t part_tiles, key_tiles, row_tiles, key_blocks, row_blocks;
     int32_t result;
     ElemFormat f;
 };
@@ -201,7 +202,7 @@ __device__ __forceinline__ void load_query_rows(AttnTile<NQ, DT, kKvRows> &t, co
 // Keys whose dK and dV a workgroup adds up over (a part of) the rows that may see them.
 struct KeyBlock {
     int b, kh, part, k0, key, rows, first, last;
-    bool live, used;
+    bool live, used, partial;
     int64_t info;
     AttnSeq seq;
 };
@@ -209,10 +210,14 @@ __device__ __forceinline__ KeyBlock key_block(const AttnBwd &a, uint32_t id, int
 {
     const AttnShape &s = a.s;
     KeyBlock k;
-    const uint32_t part = id % a.parts, tile = id / a.parts % a.key_tiles, rest = id / a.parts / a.key_tiles;
+    // tiles in parts first (they are the ones with the most rows), then the others
+    const uint32_t in_parts = a.part_tiles * a.parts, blocks = in_parts + a.key_tiles - a.part_tiles, n = id % blocks, rest = id / blocks;
+    const uint32_t tile = n < in_parts ? n / a.parts : n - in_parts + a.part_tiles, part = n < in_parts ? n % a.parts : 0u;
+    const int parts = n < in_parts ? a.parts : 1;
     k.kh = static_cast<int>(rest % s.kv_heads);
     k.b = static_cast<int>(rest / s.kv_heads);
     k.part = static_cast<int>(part);
+    k.partial = n < in_parts;
     k.k0 = static_cast<int>(tile) * kKvKeys;
     k.key = k.k0 + static_cast<int>(threadIdx.x >> 6) * 32 + static_cast<int>(threadIdx.x & 31);
     k.seq = attn_seq(s, k.b);
@@ -230,9 +235,9 @@ __device__ __forceinline__ KeyBlock key_block(const AttnBwd &a, uint32_t id, int
     if (k.k0 >= k.seq.length) t1 = 0;
     k.first = k.last = 0;
     if (t0 < t1) {                       // in tiles of `step` rows, and of these the part
-        const int64_t n0 = t0 * s.group / step, n1 = (t1 * s.group + step - 1) / step, n = n1 - n0;
-        k.first = static_cast<int>(n0 + n * k.part / a.parts) * step;
-        k.last = static_cast<int>(n0 + n * (k.part + 1) / a.parts) * step;
+        const int64_t n0 = t0 * s.group / step, n1 = (t1 * s.group + step - 1) / step, all = n1 - n0;
+        k.first = static_cast<int>(n0 + all * k.part / parts) * step;
+        k.last = static_cast<int>(n0 + all * (k.part + 1) / parts) * step;
     }
     return k;
 }
@@ -244,9 +249,9 @@ __device__ __forceinline__ void store_dkv(const AttnBwd &a, const KeyBlock &k, c
     if (!k.live) return;
     const AttnShape &s = a.s;
     const int half = (threadIdx.x & 63) >> 5;
-    const int64_t whole = static_cast<int64_t>(s.batch) * s.k_len * s.kv_heads * s.dim;
-    const int64_t at = ((static_cast<int64_t>(k.b) * s.k_len + k.key) * s.kv_heads + k.kh) * s.dim + k.part * whole;
-    const bool part = a.parts > 1;
+    const int64_t whole = static_cast<int64_t>(s.batch) * a.part_keys * s.kv_heads * s.dim;
+    const int64_t at = ((static_cast<int64_t>(k.b) * a.part_keys + k.key) * s.kv_heads + k.kh) * s.dim + k.part * whole;
+    const bool part = k.partial;
     void *kout = part ? a.part : const_cast<void *>(a.dk.p), *vout = part ? a.part + a.parts * whole : const_cast<void *>(a.dv.p);
     const int64_t kbase = part ? at : k.b * a.dk.sb + k.key * a.dk.st + k.kh * a.dk.sh;
     const int64_t vbase = part ? at : k.b * a.dv.sb + k.key * a.dv.st + k.kh * a.dv.sh;

@@ -123,7 +123,7 @@ __global__ __launch_bounds__(256) void attn_parts_kernel(AttnBwd a)
 {
     const AttnShape &s = a.s;
     const int fours = (s.dim + 3) / 4;
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, tokens = static_cast<int64_t>(s.batch) * s.k_len * s.kv_heads;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, tokens = static_cast<int64_t>(s.batch) * a.part_keys * s.kv_heads;
     if (n >= 2 * tokens * fours) return;
     const bool value = n >= tokens * fours;
     const int64_t i = value ? n - tokens * fours : n, token = i / fours, whole = tokens * s.dim;
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(256) void attn_parts_kernel(AttnBwd a)
         for (int j = 0; j < 4; ++j)
             if (j < count) v[j] += p[j];
     const AttnView &out = value ? a.dv : a.dk;
-    const int kh = static_cast<int>(token % s.kv_heads), key = static_cast<int>(token / s.kv_heads % s.k_len), b = static_cast<int>(token / s.kv_heads / s.k_len);
+    const int kh = static_cast<int>(token % s.kv_heads), key = static_cast<int>(token / s.kv_heads % a.part_keys), b = static_cast<int>(token / s.kv_heads / a.part_keys);
     store4(const_cast<void *>(out.p), b * out.sb + key * out.st + kh * out.sh + col, count, v, a.result, a.f);
 }
 
@@ -159,10 +159,24 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
     a.row_tiles = static_cast<uint32_t>(all_rows == 0 ? 0 : (rows + kRowTile - 1) / kRowTile);
     a.key_tiles = static_cast<uint32_t>((s.k_len + kKvKeys - 1) / kKvKeys);
     // few keys, many rows: their rows in parts of 256 or more, until the compute units have two workgroups each
-    const int64_t blocks = static_cast<int64_t>(a.key_tiles) * s.kv_heads * s.batch;
+    const int64_t bkh = static_cast<int64_t>(s.batch) * s.kv_heads, blocks = a.key_tiles * bkh;
     int64_t parts = blocks == 0 ? 1 : std::min((2 * cus + blocks - 1) / blocks, rows / 256);
-    a.parts = static_cast<int32_t>(std::max<int64_t>(parts, 1));
-    const int64_t key_blocks = blocks * a.parts, row_blocks = static_cast<int64_t>(a.row_tiles) * s.kv_heads * s.batch;
+    a.part_tiles = a.key_tiles;
+    if (parts <= 1) {
+        parts = 1;
+        a.part_tiles = 0;
+        // tiles with sinks, which all rows see, where the others are seen from a window: in parts of about as many rows (4 x 1024 tokens with a
+        // window of 256: the kernel 78 -> 57 us)
+        const int64_t near = (static_cast<int64_t>(s.window) + kKvKeys) * s.group;
+        if (s.window > 0 && s.sinks > 0 && rows >= 2 * near) {
+            parts = std::min(rows / near, rows / 256);
+            a.part_tiles = std::min(a.key_tiles, static_cast<uint32_t>((std::min(s.sinks, s.k_len) + kKvKeys - 1) / kKvKeys));
+            if (parts <= 1) parts = 1, a.part_tiles = 0;
+        }
+    }
+    a.parts = static_cast<int32_t>(parts);
+    a.part_keys = static_cast<int32_t>(std::min<int64_t>(s.k_len, static_cast<int64_t>(a.part_tiles) * kKvKeys));
+    const int64_t key_blocks = (a.part_tiles * parts + a.key_tiles - a.part_tiles) * bkh, row_blocks = static_cast<int64_t>(a.row_tiles) * s.kv_heads * s.batch;
     if (key_blocks + row_blocks > 0x1FFFFFFF) return FMT_ERR_SHAPE;
     a.key_blocks = static_cast<uint32_t>(key_blocks);
     a.row_blocks = static_cast<uint32_t>(row_blocks);
@@ -174,8 +188,8 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
     a.up = a.check ? kHalfUp : 1.0f;
 
     // scratch: fp16 operands first (rows of 64 or 128 bytes), then words
-    const int64_t bkh = static_cast<int64_t>(s.batch) * s.kv_heads, width = s.dim <= 64 ? 64 : 128;
-    const int64_t prows = bkh * a.row_tiles * kRowTile, pkeys = bkh * a.key_tiles * kKvKeys, whole = static_cast<int64_t>(s.batch) * s.k_len * s.kv_heads * s.dim;
+    const int64_t width = s.dim <= 64 ? 64 : 128;
+    const int64_t prows = bkh * a.row_tiles * kRowTile, pkeys = bkh * a.key_tiles * kKvKeys, whole = static_cast<int64_t>(s.batch) * a.part_keys * s.kv_heads * s.dim;
     static_assert(kRowTile / kPackRows == 4 && kKvKeys / kPackRows == 4);
     const int64_t operands = half ? (prows + pkeys) * width : 0, nhighs = half ? 4 * bkh * (a.row_tiles + 2 * a.key_tiles) : 0;      // words: two tensors of half a word
     const int64_t nparts = a.parts > 1 ? 2 * a.parts * whole : 0;

@@ -57,7 +57,8 @@ __device__ __forceinline__ void fwd_store(const AttnFwd &a, const f32x16 (&o)[DT
 // lanes l and l + 32, so the running maximum and sum of a row need one exchange per tile of 64 keys.
 // What a launch of the kernels of one head size (DT blocks of 32 columns) needs to know beside their arguments.
 struct FwdChoice {
-    bool half, two, codes, check;
+    bool half, two;           // fp16 operands, in one or two pieces of P
+    int kind;                 // kHalfCodes and so on
 };
 template <int DT>
 void run_attention_fwd(const AttnFwd &a, const FwdChoice &c, dim3 blocks, hipStream_t stream);
@@ -183,9 +184,8 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
 
 // The same on operands of one fp16 value each, P in NP pieces of fp16.  The next tile's elements are on their way from memory while a
 // tile is computed; they are rounded and converted on their way into the other of two LDS buffers, so a tile costs one barrier.
-// CHECK: the operands' range has a limit.
-template <int NP, int DT, bool CODES, bool CHECK>
-__global__ __launch_bounds__(256, DT == 2 ? (CODES ? 3 : 2) : (CODES ? 2 : 1)) void attn_fwd_half_kernel(AttnFwd a)
+template <int NP, int DT, int KIND>
+__global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (half_is_codes(KIND) ? 2 : 1)) void attn_fwd_half_kernel(AttnFwd a)
 {
     __shared__ union Shared {
         struct {
@@ -196,6 +196,7 @@ __global__ __launch_bounds__(256, DT == 2 ? (CODES ? 3 : 2) : (CODES ? 2 : 1)) v
     } sh;
     auto &ks = sh.half.ks, &vs = sh.half.vs;
     constexpr int kEights = 4 * DT, kLoads = kFwdKeys * kEights / 256;
+    constexpr bool CODES = half_is_codes(KIND);
     const AttnShape &s = a.s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const FwdBlock blk = fwd_block(a, xcd_order(blockIdx.x, gridDim.x));
@@ -210,21 +211,32 @@ __global__ __launch_bounds__(256, DT == 2 ? (CODES ? 3 : 2) : (CODES ? 2 : 1)) v
     const int64_t i1 = static_cast<int64_t>(seq.first) + (min(row0 + kFwdRows, rows) - 1) / s.group;
     uint32_t high = 0, high_value = 0;
 
-    const int64_t kbase = b * a.k.sb + kh * a.k.sh, vbase = b * a.v.sb + kh * a.v.sh;
     const AttnTiles tiles = attn_tiles(s, seq.length, i0, i1, kFwdKeys);
     const int count = tiles.count();
     const int begin = static_cast<int>(static_cast<int64_t>(count) * split / a.splits);
     const int end = static_cast<int>(static_cast<int64_t>(count) * (split + 1) / a.splits);
     RawEight<CODES> kr[kLoads], vr[kLoads];
     const int key_in = threadIdx.x / kEights, col_in = (threadIdx.x % kEights) * 8;     // + 256 / kEights keys per load
+    constexpr int kStep = 256 / kEights, kSize = CODES ? 2 : 4;
+    const char *kp = static_cast<const char *>(a.k.p) + (b * a.k.sb + kh * a.k.sh + key_in * a.k.st + col_in) * kSize;
+    const char *vp = static_cast<const char *>(a.v.p) + (b * a.v.sb + kh * a.v.sh + key_in * a.v.st + col_in) * kSize;
+    const int64_t kst = a.k.st * kSize, vst = a.v.st * kSize;
     auto fetch = [&](int n) __attribute__((always_inline)) {
         const int k0 = tiles.at(n) * kFwdKeys;
+        const char *kt = kp + k0 * kst, *vt = vp + k0 * vst;
+        if (s.dim == 32 * DT && k0 + kFwdKeys <= seq.length) {           // nothing is missing: no lane asks
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int key = k0 + key_in + i * (256 / kEights);
-            const int have = key < seq.length ? s.dim - col_in : 0;
-            kr[i] = raw_load<CODES>(a.k.p, kbase + key * a.k.st + col_in, have);
-            vr[i] = raw_load<CODES>(a.v.p, vbase + key * a.v.st + col_in, have);
+            for (int i = 0; i < kLoads; ++i) {
+                kr[i] = raw_load<CODES>(kt + i * kStep * kst, 0, 8);
+                vr[i] = raw_load<CODES>(vt + i * kStep * vst, 0, 8);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int have = k0 + key_in + i * kStep < seq.length ? s.dim - col_in : 0;
+                kr[i] = raw_load<CODES>(kt + i * kStep * kst, 0, have);
+                vr[i] = raw_load<CODES>(vt + i * kStep * vst, 0, have);
+            }
         }
     };
     if (begin < end) fetch(begin);
@@ -234,7 +246,7 @@ __global__ __launch_bounds__(256, DT == 2 ? (CODES ? 3 : 2) : (CODES ? 2 : 1)) v
     for (int kk = 0; kk < 2 * DT; ++kk) {
         const int col = 16 * kk + 8 * half;
         q[kk] = half_signed(
-            raw_half<CODES>(raw_load<CODES>(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, live ? s.dim - col : 0), a.up, a.hc, high, a.f), s.scale);
+            raw_half<KIND>(raw_load<CODES>(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, live ? s.dim - col : 0), a.up, a.hc, high, a.f), s.scale);
     }
     f32x16 o[DT];
 #pragma unroll
@@ -249,8 +261,8 @@ __global__ __launch_bounds__(256, DT == 2 ? (CODES ? 3 : 2) : (CODES ? 2 : 1)) v
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int key = key_in + i * (256 / kEights);
-            *reinterpret_cast<u32x4 *>(&ks[buf].e[0][key][col_in]) = raw_half<CODES>(kr[i], a.up, a.hc, high, a.f);
-            *reinterpret_cast<u32x4 *>(&vs[buf].e[0][key][col_in]) = raw_half<CODES>(vr[i], a.up, a.hc, high_value, a.f);
+            *reinterpret_cast<u32x4 *>(&ks[buf].e[0][key][col_in]) = raw_half<KIND>(kr[i], a.up, a.hc, high, a.f);
+            *reinterpret_cast<u32x4 *>(&vs[buf].e[0][key][col_in]) = raw_half<KIND>(vr[i], a.up, a.hc, high_value, a.f);
         }
         __syncthreads();
         if (n + 1 < end) fetch(n + 1);
@@ -310,8 +322,8 @@ __global__ __launch_bounds__(256, DT == 2 ? (CODES ? 3 : 2) : (CODES ? 2 : 1)) v
     }
     sum += __shfl_xor(sum, 32);
     const float over = sum == 0.0f ? 0.0f : 1.0f / (sum * a.up);
-    if constexpr (CHECK) {
-        if (half_flag<CODES>(high, high_value, a.hc)) {
+    if constexpr (half_has_limit(KIND)) {
+        if (a.up != 1.0f && half_flag<CODES>(high, high_value, a.hc)) {
             fwd_pieces<DT>(a, blk.id, sh.pieces);
             return;
         }
@@ -328,12 +340,19 @@ void run_attention_fwd(const AttnFwd &a, const FwdChoice &c, dim3 blocks, hipStr
         attn_fwd_kernel<DT><<<blocks, dim3(256), 0, stream>>>(a);
         return;
     }
-    auto go = [&](auto two, auto codes, auto check) {
-        attn_fwd_half_kernel<decltype(two)::value ? 2 : 1, DT, decltype(codes)::value, decltype(check)::value><<<blocks, dim3(256), 0, stream>>>(a);
+    auto go = [&](auto kind) {
+        if (c.two) attn_fwd_half_kernel<2, DT, decltype(kind)::value><<<blocks, dim3(256), 0, stream>>>(a);
+        else attn_fwd_half_kernel<1, DT, decltype(kind)::value><<<blocks, dim3(256), 0, stream>>>(a);
     };
-    auto pick = [&](auto two, auto codes) { c.check ? go(two, codes, std::true_type{}) : go(two, codes, std::false_type{}); };
-    if (c.two) c.codes ? pick(std::true_type{}, std::true_type{}) : pick(std::true_type{}, std::false_type{});
-    else c.codes ? pick(std::false_type{}, std::true_type{}) : pick(std::false_type{}, std::false_type{});
+    switch (c.kind) {
+    case kHalfCodes: go(std::integral_constant<int, kHalfCodes>{}); break;
+    case kHalfFloat: go(std::integral_constant<int, kHalfFloat>{}); break;
+    case kBf16Codes: go(std::integral_constant<int, kBf16Codes>{}); break;
+    case kSixCodes: go(std::integral_constant<int, kSixCodes>{}); break;
+    case kOtherCodes: go(std::integral_constant<int, kOtherCodes>{}); break;
+    case kMagicFloat: go(std::integral_constant<int, kMagicFloat>{}); break;
+    default: go(std::integral_constant<int, kIntegerFloat>{}); break;
+    }
 }
 
 }  // namespace fmt

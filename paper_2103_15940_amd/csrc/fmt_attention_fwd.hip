@@ -138,7 +138,7 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
         rc = launch_attention_few(s, q, k, v, o, lse, store, result, a.splits, a.part, f, fmt, stream);
         return rc != FMT_OK ? rc : launch_join(a, stream);
     }
-    const FwdChoice choice{half, half_pieces(fmt, result) == 2, a.codes, check};
+    const FwdChoice choice{half, half_pieces(fmt, result) == 2, half_kind(fmt, store)};
     const dim3 blocks(static_cast<uint32_t>(grid));
     if (s.dim <= 64) run_attention_fwd<2>(a, choice, blocks, stream);
     else run_attention_fwd<4>(a, choice, blocks, stream);

@@ -247,14 +247,20 @@ __device__ __forceinline__ f32x16 mfma_f16(u32x4 a, u32x4 b, f32x16 c)
 template <int N>
 __device__ __forceinline__ void f16_pieces(const float (&v)[8], u32x4 (&out)[N])
 {
+    float x[8];
     f16x8 hi;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) hi[i] = static_cast<_Float16>(v[i]);
+    for (int i = 0; i < 8; ++i) {
+        x[i] = v[i];
+        // where v is a product, both pieces have to be of its fp32 value: one of them taken from the product itself leaves a unit of the other out
+        if (N == 2) asm("" : "+v"(x[i]));
+        hi[i] = static_cast<_Float16>(x[i]);
+    }
     out[0] = __builtin_bit_cast(u32x4, hi);
     if constexpr (N == 2) {
         f16x8 lo;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) lo[i] = static_cast<_Float16>(__fsub_rn(v[i], static_cast<float>(hi[i])));
+        for (int i = 0; i < 8; ++i) lo[i] = static_cast<_Float16>(__fsub_rn(x[i], static_cast<float>(hi[i])));
         out[1] = __builtin_bit_cast(u32x4, lo);
     }
 }
@@ -459,16 +465,11 @@ __device__ __forceinline__ void store_row(void *y, int64_t base, int half, int d
     if (result == FMT_RESULT_F32) {
         each(floats);
     } else if (result == FMT_RESULT_CODE16 && f.codec == kCodecBf16) {
-        const uint32_t flush = f.ftz ? f.p.t_den : 0u;
+        const float flush = f.ftz ? __uint_as_float(f.p.t_den) : 0.0f;
         each([&](int col, int count, const float (&v)[4]) __attribute__((always_inline)) {
             uint16_t c[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t u = __float_as_uint(v[i]), a = u & 0x7FFFFFFFu;
-                uint32_t r = a < flush ? 0u : (a + 0x7FFFu + (a >> 16 & 1u)) >> 16;
-                r = a > 0x7F800000u ? 0x7FC0u : r | (u >> 31) << 15;
-                c[i] = static_cast<uint16_t>(r);
-            }
+            for (int i = 0; i < 4; ++i) c[i] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(fabsf(v[i]) < flush ? v[i] * 0.0f : v[i]));
             codes(col, count, c);
         });
     } else if (result == FMT_RESULT_CODE16 && f.codec == kCodecHalf) {

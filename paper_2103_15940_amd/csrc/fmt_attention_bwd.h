@@ -369,10 +369,15 @@ __global__ __launch_bounds__(256) void attn_bwd_kernel(AttnBwd a)
 // far, and sums are brought along when c falls.  A workgroup that meets a |dS| that fp16 does not hold computes again with pieces of bf16, as with
 // operands out of range.
 
-// The largest magnitudes of what a workgroup reads, as bit patterns.
+// The largest magnitudes of what a workgroup reads, as bit patterns, and of a lane's dS (NaN stays).
 struct Highs {
-    uint32_t q = 0, k = 0, v = 0, ds = 0;
+    uint32_t q = 0, k = 0, v = 0;
+    float ds = 0.0f;
 };
+__device__ __forceinline__ void track(Highs &h, float a, float b)
+{
+    h.ds = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(a), fabsf(b)), h.ds);
+}
 
 // Where attn_pack_kernel left them for one (batch, kv head).
 struct PackHighs {
@@ -395,7 +400,7 @@ struct PackHighs {
 // Whether a workgroup has to be computed with bf16 pieces: in all of its threads.
 __device__ __forceinline__ bool half_flags(const AttnBwd &a, const Highs &h)
 {
-    bool bad = h.ds > __float_as_uint(65504.0f);
+    bool bad = !(h.ds <= 65504.0f);
     if (a.check) {                                     // q, k and v are the same in the whole workgroup
         const uint32_t least = __float_as_uint(kHalfLeast);
         bad |= max(max(h.q, h.k), h.v) >= __float_as_uint(kHalfLimit);
@@ -496,9 +501,10 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float p = exp2_fast(fmaf(x[8 * kb + j], scale2, -lse2));
-                    ds[j] = p == 0.0f ? 0.0f : p * fmaf(dp[8 * kb + j], down, -delta);
-                    high.ds = max(high.ds, __float_as_uint(ds[j]) & 0x7FFFFFFFu);
+                    ds[j] = p * fmaf(dp[8 * kb + j], down, -delta);
                 }
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) track(high, ds[j], ds[j + 1]);
                 u32x4 pp[NP];
                 f16_pieces<NP>(ds, pp);
 #pragma unroll
@@ -522,7 +528,7 @@ constexpr int kHalfRows = DT == 2 ? 64 : 32;
 template <int DT>
 struct DkvHalfShared {
     AttnTile<1, DT, kHalfRows<DT>> qs[2], gs[2];
-    alignas(16) float lse[2][kHalfRows<DT>], delta[2][kHalfRows<DT>], weight[2][kHalfRows<DT>];
+    alignas(16) float lse[2][kHalfRows<DT>], delta[2][kHalfRows<DT>];
     float least[2];
 };
 
@@ -564,6 +570,7 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
 #pragma unroll
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
     const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up), down = 1.0f / a.up;
+    const float down14 = down * 0x1p-14f;
     // rows that see the lane's key
     int seen_from = 0;
     uint32_t seen = 0;
@@ -591,9 +598,9 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
             for (int w = 32; w > 0; w >>= 1) low = fminf(low, __shfl_xor(low, w));
             running = fminf(running, low);
             if (threadIdx.x < kRows) {
-                sh.lse[buf][threadIdx.x] = info[0];
-                sh.delta[buf][threadIdx.x] = info[1];
-                sh.weight[buf][threadIdx.x] = info[2] == kNoRow ? 0.0f : ldexpf(1.0f, static_cast<int>(running - info[2]));
+                // P of the row times 2^(14 + c - grow) comes out of the exponential (a row of zeros has none), and delta goes with it
+                sh.lse[buf][threadIdx.x] = info[2] == kNoRow ? INFINITY : info[0] - kProbUp - (running - info[2]);
+                sh.delta[buf][threadIdx.x] = info[1] * 0x1p-14f;
             }
             if (threadIdx.x == 0) sh.least[buf] = running;
         }
@@ -639,15 +646,13 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
                 for (int j0 = 0; j0 < 8; j0 += 4) {
                     const int row = 32 * rt + 16 * kb + 2 * j0 + 4 * half;
                     const f32x4 lse = *reinterpret_cast<const f32x4 *>(&sh.lse[buf][row]), delta = *reinterpret_cast<const f32x4 *>(&sh.delta[buf][row]);
-                    const f32x4 weight = *reinterpret_cast<const f32x4 *>(&sh.weight[buf][row]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float e = exp2_fast(fmaf(x[8 * kb + j0 + j], scale2, -lse[j])) * weight[j];
-                        const float d = e == 0.0f ? 0.0f : e * fmaf(dp[8 * kb + j0 + j], down, -delta[j]);
-                        p[j0 + j] = e * 16384.0f;
-                        ds[j0 + j] = d;
-                        high.ds = max(high.ds, __float_as_uint(d) & 0x7FFFFFFFu);
+                        p[j0 + j] = exp2_fast(fmaf(x[8 * kb + j0 + j], scale2, -lse[j]));
+                        ds[j0 + j] = p[j0 + j] * fmaf(dp[8 * kb + j0 + j], down14, -delta[j]);
                     }
+                    track(high, ds[j0], ds[j0 + 1]);
+                    track(high, ds[j0 + 2], ds[j0 + 3]);
                 }
                 u32x4 pp[NP], dd[NP];
                 f16_pieces<NP>(p, pp);

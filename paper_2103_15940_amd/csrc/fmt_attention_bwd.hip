@@ -130,10 +130,17 @@ __global__ __launch_bounds__(256) void attn_parts_kernel(AttnBwd a)
     const int col = static_cast<int>(i % fours) * 4, count = min(s.dim - col, 4);
     const float *p = a.part + (value ? a.parts * whole : 0) + token * s.dim + col;
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int part = 0; part < a.parts; ++part, p += whole)
+    for (int part0 = 0; part0 < a.parts; part0 += 8, p += 8 * whole) {
+        float x[8][4];                             // eight parts on their way at a time
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < count) v[j] += p[j];
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i][j] = part0 + i < a.parts && j < count ? p[i * whole + j] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] += x[i][j];
+    }
     const AttnView &out = value ? a.dv : a.dk;
     const int kh = static_cast<int>(token % s.kv_heads), key = static_cast<int>(token / s.kv_heads % a.part_keys), b = static_cast<int>(token / s.kv_heads / a.part_keys);
     store4(const_cast<void *>(out.p), b * out.sb + key * out.st + kh * out.sh + col, count, v, a.result, a.f);

@@ -206,22 +206,57 @@ inline int elem_kind(const ElemFormat &f)
     return f.p.mode == kModeMagic ? kKindMagic : f.p.mode == kModeInteger ? kKindInteger : kKindMixed;
 }
 
+// R of eight values.  Where all are below the threshold of infinity (a look of half an instruction each, the same in the whole wave) the short
+// forms do; with the flush, e == 8 also asks for values that it would make zero (others than 0, which a dropout leaves many of).
 template <int KIND>
 __device__ __forceinline__ void round_kind(float (&v)[8], const ElemFormat &f)
 {
     if constexpr (KIND == kKindNone) return;
-    const uint32_t flush = f.ftz ? f.p.t_den : 0u;
+    if constexpr (KIND == kKindHalf) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t u = __float_as_uint(v[i]);
-        if constexpr (KIND == kKindHalf) {
+        for (int i = 0; i < 8; ++i) {
             // the fp32 value itself is what is rounded: product and conversion in one instruction would round once, and lose the sign of -0
             asm("" : "+v"(v[i]));
             v[i] = static_cast<float>(static_cast<_Float16>(v[i]));
-        } else {
-            constexpr int kMode = KIND == kKindMagic ? kModeMagic : KIND == kKindInteger ? kModeInteger : kModeMixed;
-            const uint32_t r = quantize_bits<kMode, false>(u, f.p);
-            v[i] = __uint_as_float((u & 0x7FFFFFFFu) < flush ? u & 0x80000000u : r);
+        }
+    } else {
+        const QuantParams &p = f.p;
+        uint32_t u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(v[i]);
+        if constexpr (KIND != kKindMixed) {
+            bool rare = run_is_rare(u, p);
+            if constexpr (KIND == kKindInteger) {
+                if (f.ftz) {
+                    uint32_t low = 0xFFFFFFFFu;
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2) low = min(min((u[i] << 1) - 1u, (u[i + 1] << 1) - 1u), low);
+                    rare |= low < (p.t_den << 1) - 1u;
+                }
+            }
+            if (!__any(rare)) {
+                if constexpr (KIND == kKindInteger) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float((u[i] + p.rbias + __builtin_amdgcn_ubfe(u[i], p.shift, p.lsb_width)) & p.nmask);
+                } else {
+                    const RoundMasks k = round_masks(p);
+                    if (f.ftz) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(quantize_short<kModeMagic, true>(u[i], p, k));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(quantize_short<kModeMagic, false>(u[i], p, k));
+                    }
+                }
+                return;
+            }
+        }
+        constexpr int kMode = KIND == kKindMagic ? kModeMagic : KIND == kKindInteger ? kModeInteger : kModeMixed;
+        const uint32_t flush = f.ftz ? p.t_den : 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t r = quantize_bits<kMode, false>(u[i], p);
+            v[i] = __uint_as_float((u[i] & 0x7FFFFFFFu) < flush ? u[i] & 0x80000000u : r);
         }
     }
 }

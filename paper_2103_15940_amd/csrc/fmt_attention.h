@@ -243,24 +243,24 @@ __device__ __forceinline__ f32x16 mfma_f16(u32x4 a, u32x4 b, f32x16 c)
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// Eight fp32 values as N fp16 pieces, to nearest: 11 or 22 bits, and nothing below 2^-25.
+// Eight fp32 values as N fp16 pieces: 11 bits, to nearest, or 22, the first of them cut (its rest goes into the second, to nearest).
 template <int N>
 __device__ __forceinline__ void f16_pieces(const float (&v)[8], u32x4 (&out)[N])
 {
-    float x[8];
-    f16x8 hi;
+    if constexpr (N == 1) {
+        f16x8 h;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x[i] = v[i];
-        // where v is a product, both pieces have to be of its fp32 value: one of them taken from the product itself leaves a unit of the other out
-        if (N == 2) asm("" : "+v"(x[i]));
-        hi[i] = static_cast<_Float16>(x[i]);
-    }
-    out[0] = __builtin_bit_cast(u32x4, hi);
-    if constexpr (N == 2) {
+        for (int i = 0; i < 8; ++i) h[i] = static_cast<_Float16>(v[i]);
+        out[0] = __builtin_bit_cast(u32x4, h);
+    } else {
         f16x8 lo;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) lo[i] = static_cast<_Float16>(__fsub_rn(x[i], static_cast<float>(hi[i])));
+        for (int i = 0; i < 8; i += 2) {
+            const auto hi = __builtin_amdgcn_cvt_pkrtz(v[i], v[i + 1]);
+            out[0][i / 2] = __builtin_bit_cast(uint32_t, hi);
+            lo[i] = static_cast<_Float16>(__fsub_rn(v[i], static_cast<float>(hi[0])));
+            lo[i + 1] = static_cast<_Float16>(__fsub_rn(v[i + 1], static_cast<float>(hi[1])));
+        }
         out[1] = __builtin_bit_cast(u32x4, lo);
     }
 }
@@ -399,8 +399,10 @@ __device__ __forceinline__ u32x4 half_signed(u32x4 q, float scale)
     return q;
 }
 
-// P is taken times 2^14, so that its fp16 pieces hold their bits down to P = 2^-28.
-constexpr float kProbUp = 14.0f;
+// Backward, P is taken times 2^14, so that its fp16 pieces hold their bits down to P = 2^-28.  Forward the running maximum stays where it is
+// until a score passes it by 2^8 (a wave of 32 rows would otherwise multiply its sums with some row's factor at almost every tile), so P can
+// reach 2^8, and is taken times 2^6.
+constexpr float kProbUp = 14.0f, kFwdUp = 6.0f, kFwdSlack = 8.0f;
 
 // Whether a workgroup has to be computed with bf16 pieces: in all of its threads.  Every thread calls it.  high, high_value: what raw_half left.
 template <bool CODES>

@@ -268,16 +268,15 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
         if (n + 1 < end) fetch(n + 1);
         f32x16 x[2];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
+        for (int i = 0; i < 16; ++i) x[0][i] = x[1][i] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[kt][i] = 0.0f;
+        for (int kk = 0; kk < 2 * DT; ++kk)
 #pragma unroll
-            for (int kk = 0; kk < 2 * DT; ++kk) {
+            for (int kt = 0; kt < 2; ++kt) {              // two sums in turn: a product does not wait for the one before it
                 u32x4 f[1];
                 read_rows(ks[buf], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
                 x[kt] = mfma_f16(f[0], q[kk], x[kt]);
             }
-        }
         if (!attn_sees_all(s, seq.length, i0, i1, k0, k0 + kFwdKeys)) {
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) attn_hide(sees, k0 + 32 * kt + 4 * half, x[kt]);
@@ -288,7 +287,7 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
 #pragma unroll
             for (int i = 0; i < 16; ++i) high_score = fmaxf(high_score, x[kt][i]);
         high_score = fmaxf(high_score, __shfl_xor(high_score, 32)) * scale2;
-        if (__any(high_score > top)) {                    // else the running maximum stays in all of the wave's rows
+        if (__any(high_score > top + kFwdSlack)) {
             const float next = fmaxf(top, high_score);
             const float shrink = next == -INFINITY ? 1.0f : exp2_fast(top - next);
             top = next;
@@ -298,7 +297,7 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= shrink;
         }
-        const float base = (top == -INFINITY ? 0.0f : top) - kProbUp;
+        const float base = (top == -INFINITY ? 0.0f : top) - kFwdUp;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -328,7 +327,7 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
             return;
         }
     }
-    if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, sum == 0.0f ? -INFINITY : top - kProbUp + log2f(sum));
+    if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, sum == 0.0f ? -INFINITY : top - kFwdUp + log2f(sum));
 }
 
 }  // namespace

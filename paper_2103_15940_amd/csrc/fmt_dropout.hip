@@ -17,13 +17,31 @@ __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const void *x, in
     RawEight<CODES> raw[kDropRuns];
     int64_t to[kDropRuns];
     int count[kDropRuns];
+    const uint32_t past0 = at0 + threadIdx.x, over0 = past0 / blocks;
+    uint32_t g = past0 - over0 * blocks;                  // the eight's place in its row
+    int64_t xo = static_cast<int64_t>(row0 + over0) * ldx + static_cast<int64_t>(g) * 8, yo = static_cast<int64_t>(row0 + over0) * ldy + static_cast<int64_t>(g) * 8;
 #pragma unroll
     for (int i = 0; i < kDropRuns; ++i) {
-        const uint32_t step = threadIdx.x + kDropThreads * i, past = at0 + step, over = past / blocks, g = past - over * blocks;
-        const int64_t row = static_cast<int64_t>(row0 + over), col = static_cast<int64_t>(g) * 8;
-        count[i] = first + step < total ? static_cast<int>(cols - col < 8 ? cols - col : 8) : 0;
-        to[i] = row * ldy + col;
-        raw[i] = raw_load<CODES>(x, row * ldx + col, count[i]);
+        const int64_t left = cols - static_cast<int64_t>(g) * 8;
+        count[i] = first + threadIdx.x + kDropThreads * i < total ? static_cast<int>(left < 8 ? left : 8) : 0;
+        to[i] = yo;
+        raw[i] = raw_load<CODES>(x, xo, count[i]);
+        // on by 256 eights: the vector units have no division, and multiply 64 bits in a dozen steps
+        g += kDropThreads;
+        xo += 8 * kDropThreads;
+        yo += 8 * kDropThreads;
+        if (blocks >= kDropThreads) {
+            if (g >= blocks) {
+                g -= blocks;
+                xo += ldx - 8 * static_cast<int64_t>(blocks);
+                yo += ldy - 8 * static_cast<int64_t>(blocks);
+            }
+        } else {
+            const uint32_t over = g / blocks;
+            g -= over * blocks;
+            xo += over * (ldx - 8 * static_cast<int64_t>(blocks));
+            yo += over * (ldy - 8 * static_cast<int64_t>(blocks));
+        }
     }
     const DropKey key = drop_key(d);
 #pragma unroll

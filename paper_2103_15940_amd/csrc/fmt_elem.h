@@ -278,22 +278,26 @@ template <int KIND>
 __device__ __forceinline__ u32x4 encode_kind(const float (&v)[8], const ElemFormat &f)
 {
     u32x4 w;
+    float top = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
         uint32_t c[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const float x = v[i + j];
-            if constexpr (KIND == kKindHalf) {
-                const uint16_t h = __builtin_bit_cast(uint16_t, static_cast<_Float16>(x));
-                c[j] = x != x ? 0x7E00u : h;
-            } else if constexpr (KIND == kKindInteger) {
-                c[j] = __float_as_uint(x) >> (31u - f.p.sign_pos);
-            } else {
-                c[j] = encode_bits<kModeMagic>(__float_as_uint(x), f.p);
-            }
+            if constexpr (KIND == kKindHalf) c[j] = __builtin_bit_cast(uint16_t, static_cast<_Float16>(x));
+            else if constexpr (KIND == kKindInteger) c[j] = __float_as_uint(x) >> (31u - f.p.sign_pos);
+            else c[j] = encode_bits<kModeMagic>(__float_as_uint(x), f.p);
         }
         w[i / 2] = c[0] | c[1] << 16;
+        if (KIND == kKindHalf) top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(v[i]), fabsf(v[i + 1])), top);
+    }
+    if constexpr (KIND == kKindHalf) {
+        if (__any(top != top)) {                          // any NaN has one code
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (v[i] != v[i]) w[i / 2] = (w[i / 2] & (i & 1 ? 0x0000FFFFu : 0xFFFF0000u)) | 0x7E00u << (16 * (i & 1));
+        }
     }
     return w;
 }

@@ -503,6 +503,17 @@ __device__ __forceinline__ void store_row(void *y, int64_t base, int half, int d
     }
 }
 
+// Up to four neighbouring values of a part.
+__device__ __forceinline__ f32x4 load4(const float *p, int count)
+{
+    if (count >= 4) return *reinterpret_cast<const f32x4_any *>(p);
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < count) v[i] = p[i];
+    return v;
+}
+
 // Up to four neighbouring results of kernels that join parts.
 __device__ __forceinline__ void store4(void *y, int64_t at, int count, const float (&v)[4], int result, const ElemFormat &f)
 {

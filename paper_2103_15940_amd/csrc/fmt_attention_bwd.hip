@@ -131,11 +131,9 @@ __global__ __launch_bounds__(256) void attn_parts_kernel(AttnBwd a)
     const float *p = a.part + (value ? a.parts * whole : 0) + token * s.dim + col;
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int part0 = 0; part0 < a.parts; part0 += 8, p += 8 * whole) {
-        float x[8][4];                             // eight parts on their way at a time
+        f32x4 x[8];                                // eight parts on their way at a time
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[i][j] = part0 + i < a.parts && j < count ? p[i * whole + j] : 0.0f;
+        for (int i = 0; i < 8; ++i) x[i] = load4(p + i * whole, part0 + i < a.parts ? count : 0);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll

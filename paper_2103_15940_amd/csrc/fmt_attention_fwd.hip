@@ -22,13 +22,13 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnFwd a)
     const int64_t at = n / fours;
     const int col = static_cast<int>(n % fours) * 4, count = min(s.dim - col, 4);
     const float *lse = a.part + a.splits * all_rows * s.dim + at;
-    float l[kJoinFew], o[kJoinFew][4], top = -INFINITY, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 o[kJoinFew];
+    float l[kJoinFew], top = -INFINITY, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < kJoinFew; ++i) {
         const bool there = i < a.splits;
         l[i] = there ? lse[i * all_rows] : -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[i][j] = there && j < count ? a.part[(i * all_rows + at) * s.dim + col + j] : 0.0f;
+        o[i] = load4(a.part + (i * all_rows + at) * s.dim + col, there ? count : 0);
     }
 #pragma unroll
     for (int i = 0; i < kJoinFew; ++i) top = fmaxf(top, l[i]);

@@ -314,3 +314,53 @@ def test_arguments_are_checked_before_the_gpu():
     assert bwd(lddz=7) == SHAPE and bwd(dx=r, lddx=7) == SHAPE and bwd(cols=32769) == SHAPE and bwd(dz=b + 2) == ALIGN
     assert bwd(dz=a) == ALIAS and bwd(dx=b, lddx=8) == ALIAS and bwd(dgamma=r, dbeta=r + 16) == ALIAS
     assert bwd(rows=0, dy=None, z=None, mean=None, rstd=None, dz=None) == OK and bwd(store=5) == RANGE
+
+
+@gpu
+@pytest.mark.parametrize("f", FORMATS + [(7, 8, True), (3, 4, False), (8, 4, False)])
+@pytest.mark.parametrize("rows,cols", [(5, 100), (3, 1030), (2, 9000)])
+@pytest.mark.parametrize("codes", [False, True])
+def test_norm_in_every_format(fmt, f, rows, cols, codes):
+    """Every way of rounding, tensors in fp32 and in codes, with values that overflow and underflow the format."""
+    if codes and f[0] + f[1] > 15:
+        pytest.skip("the format has no 16-bit codes")
+    x, res, gamma, beta = norm_inputs(rows, cols, 3)
+    if f[0] >= 4:
+        x[0, ::7] *= np.float32(2.0 ** -20)
+    state = fmt.new_rng(3)
+    (xt, _), (rt, _) = store(fmt, x, f, codes), store(fmt, res, f, codes)
+    for result in ("f32", "round") + (("code16",) if f[0] + f[1] <= 15 else ()):
+        y, z, mean, rstd = fmt.fmt_layernorm_fwd(xt, dev(gamma), dev(beta), f, residual=rt, p=0.25, rng=state, site=1, result=result)
+        zin = L.norm_input(x, res, L.drop_mask(rows, cols, 0.25, 3, 0, 1), f)
+        assert same_bits(values(fmt, z, f, result), zin)
+        g, b = L.rounded(gamma, f).astype(np.float64), L.rounded(beta, f).astype(np.float64)
+        want, m, r = L.norm_fwd(zin, g, b, float(np.float32(1e-5)))
+        top = np.abs(zin).max(1).astype(np.float64)
+        xhat = (zin - m[:, None]) * r[:, None]
+        tol = np.abs(g) * (48 * U * top[:, None] * r[:, None] + 40 * U * np.abs(xhat)) + 2 * U * (np.abs(want) + np.abs(b))
+        close(values(fmt, y, f, result), want, tol, f, result, "y")
+        if result == "code16" and codes:
+            dz, dx, dgamma, dbeta = fmt.fmt_layernorm_bwd(rt, z, mean, rstd, dev(gamma), f, p=0.25, rng=state, site=1)
+            d = L.rounded(res, f).astype(np.float64)
+            want, wg, wb = L.norm_bwd(d, zin, mean.cpu().numpy(), rstd.cpu().numpy(), g)
+            gx = d * g
+            tol = r[:, None] * (4 * U * np.abs(gx) + 50 * U * np.abs(gx).mean(1, keepdims=True) + 64 * U * np.abs(xhat) *
+                                np.abs(gx * xhat).mean(1, keepdims=True)) * (1 + 2.0 ** -10) + 2 * U * np.abs(want)
+            close(values(fmt, dz, f, "code16"), want, tol, f, "code16", "dz")
+
+
+@gpu
+def test_dropout_past_32_bits_of_elements(fmt):
+    """More than 2^32 elements: the last rows' mask is that of their own blocks, not of blocks 2^32 back."""
+    f = (8, 7, False)
+    rows, cols = 131080, 32768
+    x = torch.ones(rows, cols, dtype=torch.bfloat16, device="cuda")
+    state = fmt.new_rng(21, 2)
+    fmt.fmt_dropout(x, 0.5, state, f, site=4, out=x)
+    tail = x[-3:].float().cpu().numpy()
+    n0 = (rows - 3) * (cols // 8)
+    n = np.arange(n0, n0 + 3 * (cols // 8), dtype=np.uint64)
+    full = lambda v: np.full(n.shape, v, dtype=np.uint64)  # noqa: E731
+    w = L.philox([n & np.uint64(0xFFFFFFFF), n >> np.uint64(32), full(2), full(4)], [21, 0])
+    bits = np.stack([(w[i // 2] >> np.uint64(16 * (i % 2))) & np.uint64(0xFFFF) for i in range(8)], 1).reshape(3, cols)
+    assert np.array_equal(tail != 0, bits >= 32768) and set(np.unique(tail)) == {0.0, 2.0}

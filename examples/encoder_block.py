@@ -96,7 +96,7 @@ def main():
         dy = (y - target) * (2.0 / y.numel()) * 1024.0                      # loss scale 1024
         _, grads = block.backward(dy, kept, f)
         for name, grad in grads.items():
-            block.weights[name] -= 20.0 / 1024.0 * grad
+            block.weights[name] -= 2.0 / 1024.0 * grad
         rng[1] += 1
         torch.cuda.synchronize()
         print("step %d: loss %.4f, %.2f ms" % (step, float((y - target).square().mean()), (time.perf_counter() - began) * 1e3), flush=True)

@@ -8,8 +8,9 @@
 // kernel joins them. All of it is fp32: any operand of any format is exact.
 //
 // Codes become fp32 by their bits: sign, and exponent field and mantissa at the place of fp32's, times 2^(127 - bias); the code's denormals are
-// fp32 denormals then, and right too. For 1/6/9 the factors are left to Q (2^64), the scale (2^32) and the outputs (2^96), and P is
-// taken times 2^64, so that sums stay among the normal numbers.
+// fp32 denormals then, and right too. For 1/6/9 the factors are left to Q (2^64), the scale (2^32) and the outputs (2^96), and P meets V
+// times 2^64, so that sums stay among the normal numbers: multiplied after the exponential, since a 64 added in its argument would
+// take five bits from it.
 #include <algorithm>
 #include <type_traits>
 
@@ -25,7 +26,7 @@ struct AttnFew {
     float *lse;               // [batch][heads][q_len]
     int32_t result, splits;
     bool codes;
-    float *part;              // splits > 1: [splits][batch * heads * q_len][dim] normalised outputs, then as many lse in base 2
+    float *part;              // splits > 1: [splits][batch * heads * q_len][dim] normalised outputs, then as many maxima in base 2, then sums
     float factor;             // 2^(127 - bias)
     uint32_t body;            // magnitude bits of a code, in both halves of a word
     ElemFormat f;
@@ -124,22 +125,21 @@ __global__ __launch_bounds__(256, R <= 1 ? 4 : R <= 4 ? 3 : 2) void attn_few_ker
     if (begin < end) fetch(begin);
     float q[R][8], o[R][8], top[R], sum[R];
     AttnKeys sees[R];
+    // Q takes the scale's sign, so that products are ordered as the scores are; a scale of 0 makes Q zero
+    const float scale2 = s.scale2 == 0.0f ? 1.0f : fabsf(s.scale2) * (KIND == kFewSix ? 0x1p32f : 1.0f);
+    const float sign = (KIND == kFewSix ? 0x1p64f : 1.0f) * (s.scale2 > 0.0f ? 1.0f : s.scale2 < 0.0f ? -1.0f : 0.0f);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int t = r / s.group, head = kh * s.group + r % s.group;
 #pragma unroll
         for (int j = 0; j < 8; ++j) q[r][j] = o[r][j] = 0.0f;
         if (r < rows && have > 0) load8_any(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, min(have, 8), q[r], a.codes, a.f);
-        if constexpr (KIND == kFewSix) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q[r][j] *= 0x1p64f;
-        }
+        for (int j = 0; j < 8; ++j) q[r][j] *= sign;
         top[r] = -INFINITY;
         sum[r] = 0.0f;
         sees[r] = attn_keys(s, seq.length, seq.first + t);
     }
-    const float scale2 = KIND == kFewSix ? s.scale2 * 0x1p32f : s.scale2;
-    constexpr float UP = KIND == kFewSix ? 64.0f : 0.0f;
     uint32_t high = 0;
     for (int n = begin; n < end; ++n) {
         const int tile0 = tiles.at(n) * TILE, k0 = tile0 + mine;
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256, R <= 1 ? 4 : R <= 4 ? 3 : 2) void attn_few_ker
                 float d = k[0] * q[r][0];
 #pragma unroll
                 for (int j = 1; j < 8; ++j) d = fmaf(k[j], q[r][j], d);
-                x[u][r] = lanes_sum<LANES>(d) * scale2;
+                x[u][r] = lanes_sum<LANES>(d);
             }
             few_values<KIND>(vr[u], v[u], a, high);
         }
@@ -173,15 +173,16 @@ __global__ __launch_bounds__(256, R <= 1 ? 4 : R <= 4 ? 3 : 2) void attn_few_ker
             float next = top[r];
 #pragma unroll
             for (int u = 0; u < U; ++u) next = fmaxf(next, x[u][r]);
-            const float base = next == -INFINITY ? 0.0f : next, shrink = exp2_fast(top[r] - base);
+            const float base = next == -INFINITY ? 0.0f : next * scale2, shrink = exp2_fast(fmaf(top[r], scale2, -base));
             top[r] = next;
             sum[r] *= shrink;
 #pragma unroll
             for (int j = 0; j < 8; ++j) o[r][j] *= shrink;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const float p = exp2_fast(x[u][r] - (base - UP));
+                float p = exp2_fast(fmaf(x[u][r], scale2, -base));
                 sum[r] += p;
+                if constexpr (KIND == kFewSix) p *= 0x1p64f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) o[r][j] = fmaf(p, v[u][j], o[r][j]);
             }
@@ -196,7 +197,7 @@ __global__ __launch_bounds__(256, R <= 1 ? 4 : R <= 4 ? 3 : 2) void attn_few_ker
 #pragma unroll
         for (int j = 0; j < 8; j += 4) *reinterpret_cast<f32x4 *>(&outs[at][r][col + j]) = f32x4{o[r][j], o[r][j + 1], o[r][j + 2], o[r][j + 3]};
         if (lane % LANES == 0) {
-            tops[at][r] = top[r];
+            tops[at][r] = top[r] * scale2;
             sums[at][r] = sum[r];
         }
     }
@@ -217,19 +218,21 @@ __global__ __launch_bounds__(256, R <= 1 ? 4 : R <= 4 ? 3 : 2) void attn_few_ker
             out = fmaf(w, outs[i][r][c], out);
         }
         if (bad) total = out = NAN;
-        if constexpr (KIND == kFewSix) out *= 0x1p64f;
         out = total == 0.0f ? 0.0f : out / total;
         if constexpr (KIND == kFewSix) out *= 0x1p32f;
-        const float lse2 = total == 0.0f ? -INFINITY : high_top - UP + log2f(total);
         const int t = r / s.group, head = kh * s.group + r % s.group;
         const int64_t row = (static_cast<int64_t>(b) * s.heads + head) * s.q_len + t;
         if (a.splits > 1) {
             a.part[(split * all_rows + row) * s.dim + c] = out;
-            if (c == 0) a.part[a.splits * all_rows * s.dim + split * all_rows + row] = lse2;
+            if (c == 0) {
+                float *records = a.part + a.splits * all_rows * s.dim + split * all_rows + row;
+                records[0] = high_top;
+                records[a.splits * all_rows] = total;
+            }
         } else {
             const float y[4] = {out, 0.0f, 0.0f, 0.0f};
             store4(const_cast<void *>(a.o.p), b * a.o.sb + t * a.o.st + head * a.o.sh + c, 1, y, a.result, a.f);
-            if (c == 0 && a.lse) a.lse[row] = lse2 * 0.6931471805599453f;
+            if (c == 0 && a.lse) a.lse[row] = total == 0.0f ? -INFINITY : (high_top + log2f(total)) * 0.6931471805599453f;
         }
     }
 }

@@ -12,7 +12,7 @@ struct AttnFwd {
     float *lse;               // [batch][heads][q_len]
     int32_t result;
     int32_t splits;           // parts of a row's keys
-    float *part;              // splits > 1: [splits][batch * heads * q_len][dim] normalised outputs, then as many lse in base 2
+    float *part;              // splits > 1: [splits][batch * heads * q_len][dim] normalised outputs, then as many maxima in base 2, then sums
     float up;                 // what the fp16 operands are multiplied by
     int32_t row_tiles;
     bool codes;               // how q, k and v are stored
@@ -38,7 +38,7 @@ __device__ __forceinline__ FwdBlock fwd_block(const AttnFwd &a, uint32_t id)
 
 // A lane's outputs: its row of a wave's results, over its sum.
 template <int DT>
-__device__ __forceinline__ void fwd_store(const AttnFwd &a, const f32x16 (&o)[DT], int split, int b, int t, int head, int half, float over, float lse2)
+__device__ __forceinline__ void fwd_store(const AttnFwd &a, const f32x16 (&o)[DT], int split, int b, int t, int head, int half, float over, float top, float sum)
 {
     const AttnShape &s = a.s;
     const int64_t at = (static_cast<int64_t>(b) * s.heads + head) * s.q_len + t;
@@ -49,8 +49,13 @@ __device__ __forceinline__ void fwd_store(const AttnFwd &a, const f32x16 (&o)[DT
     const int result = part ? FMT_RESULT_F32 : a.result;
     store_row<DT>(out, base, half, s.dim, o, over, result, a.f);
     if (half != 0) return;
-    if (part) a.part[a.splits * all_rows * s.dim + split * all_rows + at] = lse2;
-    else if (a.lse) a.lse[at] = lse2 * 0.6931471805599453f;
+    if (part) {
+        float *records = a.part + a.splits * all_rows * s.dim + split * all_rows + at;
+        records[0] = top;
+        records[a.splits * all_rows] = sum;
+    } else if (a.lse) {
+        a.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+    }
 }
 
 // A workgroup takes 128 rows of one (batch, kv head), a wave 32 of them: S^T = K Q^T gives every lane one row's scores, half of them each for
@@ -172,7 +177,7 @@ __device__ __forceinline__ void fwd_pieces(const AttnFwd &a, uint32_t id, FwdSha
     }
     sum += __shfl_xor(sum, 32);
     const float over = sum == 0.0f ? 0.0f : 1.0f / sum;          // a row that sees nothing: 0
-    if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, sum == 0.0f ? -INFINITY : top + log2f(sum));
+    if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, top, sum);
 }
 
 template <int DT>
@@ -327,7 +332,7 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
             return;
         }
     }
-    if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, sum == 0.0f ? -INFINITY : top - kFwdUp + log2f(sum));
+    if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, top - kFwdUp, sum);
 }
 
 }  // namespace

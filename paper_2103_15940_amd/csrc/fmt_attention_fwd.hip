@@ -10,7 +10,9 @@ extern template void run_attention_fwd<4>(const AttnFwd &, const FwdChoice &, di
 
 namespace {
 
-// Joins the parts of a row where they are few: a thread takes four columns, and reads all parts' lse and columns at once (a wave per row,
+// Parts of a row's keys leave their maximum and sum apart, not the lse: that, rounded, would put 2^-22 of its size into every weight.
+//
+// Joins the parts of a row where they are few: a thread takes four columns, and reads all parts' records and columns at once (a wave per row,
 // which waited for one after the other, took 10 us for 14000 rows).
 constexpr int kJoinFew = 8;
 __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnFwd a)
@@ -21,13 +23,14 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnFwd a)
     if (n >= all_rows * fours) return;
     const int64_t at = n / fours;
     const int col = static_cast<int>(n % fours) * 4, count = min(s.dim - col, 4);
-    const float *lse = a.part + a.splits * all_rows * s.dim + at;
+    const float *tops = a.part + a.splits * all_rows * s.dim + at, *sums = tops + a.splits * all_rows;
     f32x4 o[kJoinFew];
-    float l[kJoinFew], top = -INFINITY, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float l[kJoinFew], part_sum[kJoinFew], top = -INFINITY, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < kJoinFew; ++i) {
         const bool there = i < a.splits;
-        l[i] = there ? lse[i * all_rows] : -INFINITY;
+        l[i] = there ? tops[i * all_rows] : -INFINITY;
+        part_sum[i] = there ? sums[i * all_rows] : 0.0f;
         o[i] = load4(a.part + (i * all_rows + at) * s.dim + col, there ? count : 0);
     }
 #pragma unroll
@@ -35,7 +38,7 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnFwd a)
     const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
     for (int i = 0; i < kJoinFew; ++i) {
-        const float w = exp2_fast(l[i] - base);
+        const float w = part_sum[i] * exp2_fast(l[i] - base);
         sum += w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = fmaf(w, o[i][j], v[j]);
@@ -52,27 +55,27 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnFwd a)
 constexpr int kJoinMost = 2048, kJoinThreads = 1024, kJoinWaves = kJoinThreads / 64;
 __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnFwd a)
 {
-    __shared__ float weights[kJoinMost], outs[kJoinThreads], tops[kJoinWaves], sums[kJoinWaves];
+    __shared__ float weights[kJoinMost], outs[kJoinThreads], wave_tops[kJoinWaves], wave_sums[kJoinWaves];
     const AttnShape &s = a.s;
     const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len, at = blockIdx.x;
-    const float *lse = a.part + a.splits * all_rows * s.dim + at;
+    const float *tops = a.part + a.splits * all_rows * s.dim + at, *sums = tops + a.splits * all_rows;
     float top = -INFINITY, sum = 0.0f;
-    for (int n = threadIdx.x; n < a.splits; n += kJoinThreads) top = fmaxf(top, weights[n] = lse[n * all_rows]);
+    for (int n = threadIdx.x; n < a.splits; n += kJoinThreads) top = fmaxf(top, weights[n] = tops[n * all_rows]);
 #pragma unroll
     for (int w = 32; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    if ((threadIdx.x & 63) == 0) wave_tops[threadIdx.x >> 6] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kJoinWaves; ++w) top = fmaxf(top, tops[w]);
+    for (int w = 0; w < kJoinWaves; ++w) top = fmaxf(top, wave_tops[w]);
     const float base = top == -INFINITY ? 0.0f : top;
-    for (int n = threadIdx.x; n < a.splits; n += kJoinThreads) sum += weights[n] = exp2_fast(weights[n] - base);
+    for (int n = threadIdx.x; n < a.splits; n += kJoinThreads) sum += weights[n] = sums[n * all_rows] * exp2_fast(weights[n] - base);
 #pragma unroll
     for (int w = 32; w > 0; w >>= 1) sum += __shfl_xor(sum, w);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+    if ((threadIdx.x & 63) == 0) wave_sums[threadIdx.x >> 6] = sum;
     __syncthreads();
     sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kJoinWaves; ++w) sum += sums[w];
+    for (int w = 0; w < kJoinWaves; ++w) sum += wave_sums[w];
     const int width = s.dim <= 64 ? 64 : 128, groups = kJoinThreads / width, c = threadIdx.x % width, g = threadIdx.x / width;
     float o = 0.0f;
     if (c < s.dim) {
@@ -131,7 +134,7 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
     const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len, grid = work * splits;
     if (grid > 0x7FFFFFFF) return FMT_ERR_SHAPE;
     if (splits > 1) {
-        rc = get_acc_scratch(stream, static_cast<size_t>(splits * all_rows * (s.dim + 1)) * sizeof(float), &a.part);
+        rc = get_acc_scratch(stream, static_cast<size_t>(splits * all_rows * (s.dim + 2)) * sizeof(float), &a.part);
         if (rc != FMT_OK) return rc;
     }
     if (few) {

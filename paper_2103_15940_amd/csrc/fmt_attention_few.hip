@@ -173,7 +173,10 @@ __global__ __launch_bounds__(256, R <= 1 ? 4 : R <= 4 ? 3 : 2) void attn_few_ker
             float next = top[r];
 #pragma unroll
             for (int u = 0; u < U; ++u) next = fmaxf(next, x[u][r]);
-            const float base = next == -INFINITY ? 0.0f : next * scale2, shrink = exp2_fast(fmaf(top[r], scale2, -base));
+            // the maximum's product is rounded once, for all uses: an unrounded one in one of them, times all tiles, is a drift
+            float before = top[r] * scale2, base = next == -INFINITY ? 0.0f : next * scale2;
+            asm("" : "+v"(before), "+v"(base));
+            const float shrink = exp2_fast(before - base);
             top[r] = next;
             sum[r] *= shrink;
 #pragma unroll

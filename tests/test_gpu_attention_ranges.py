@@ -112,3 +112,25 @@ def test_offsets_past_32_bits_backward(fmt):  # noqa: F811
     for s, t in zip(fmt.fmt_attention_bwd(store[3], store[0], view(0), view(64), o, lse, f, causal=True),
                     fmt.fmt_attention_bwd(store[3], *store[:3], o, lse, f, causal=True)):
         assert torch.equal(s, t)
+
+
+@pytest.mark.parametrize("f,codes", [(SIX, True), (SIX, False), (BF16, True)])
+@pytest.mark.parametrize("h", [4, 16, 32])
+def test_no_drift_over_many_keys(fmt, f, codes, h):  # noqa: F811
+    """A part's running sums pass over thousands of keys: their error is that of random roundings, not one that grows with every tile.
+    A score has an error of a few 2^-24, a weight's is as large, and n additions to a sum of random signs put sqrt(n / 2) 2^-25 beside it,
+    n = 8191 / 16 keys to a lane at most: 2^-20 in all."""
+    g = torch.Generator(device="cuda").manual_seed(h)
+    b, n, hk, d = 48, 8191, 4, 64
+    q, k, v = (torch.randn(s, generator=g, device="cuda") for s in ((b, 1, h, d), (b, n, hk, d), (b, n, hk, d)))
+    t = [fmt.fmt_quantize(x.reshape(-1, d), f).view(x.shape) for x in (1.5 * q, k, v)]
+    o, lse = fmt.fmt_attention_fwd(*(fmt.fmt_pack16(x, f) if codes else x for x in t), f, result="f32")
+    wrong, size = 0.0, 0.0
+    for i in range(0, b, 12):
+        qd, kd, vd = (x[i].double().cpu() for x in t)
+        s = torch.matmul(qd.view(hk, h // hk, d), kd.permute(1, 2, 0).contiguous()) * 0.125
+        want = torch.matmul(torch.softmax(s, 2), vd.transpose(0, 1).contiguous()).view(h, d)
+        wrong += float((o[i, 0].double().cpu() - want).square().sum())
+        size += float(want.square().sum())
+        assert float((lse[i].view(hk, h // hk).double().cpu() - torch.logsumexp(s, 2)).abs().max()) <= 2.0 ** -20
+    assert wrong ** 0.5 <= 2.0 ** -20 * size ** 0.5

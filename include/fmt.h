@@ -636,6 +636,8 @@ int fmt_attention_fwd(fmt_attention_t a, fmt_view_t q, fmt_view_t k, fmt_view_t 
  *   dQ = scale * dS R(K),  dK = scale * dS^T R(Q),  dV = P^T R(dO)   (dK and dV: sums over the query heads that share them)
  *   o, lse   what the forward call gave; o, d_o, dq, dk and dv are stored as `result` says (codes, or fp32; d_o in fp32 is
  *            rounded as it is read, o is not), q, k, v as `store` says
+ *            (delta is that of o as it is stored: an o rounded to the format puts its rounding, times |dO|, into every dS of its
+ *            row; FMT_RESULT_F32 in both calls keeps it out)
  * dk and dv are [batch][k_len][kv_heads][dim]; rows from `length` on are zero.
  */
 int fmt_attention_bwd(fmt_attention_t a, fmt_view_t q, fmt_view_t k, fmt_view_t v, fmt_view_t o, fmt_view_t d_o,
@@ -666,7 +668,8 @@ int fmt_format_thresholds(fmt_format_t f, uint32_t *out);
  * fmt_scratch_bytes -- bytes of library-owned scratch that the current device holds for `stream`
  * right now: out[0] partial statistics records, out[1] the product workspace (prepared operands of
  * fmt_gemm / fmt_linear / the convolutions, rounded convolution tensors, split-k partial sums),
- * out[2] the accumulators of fmt_linear_pack16.  out is a HOST pointer to three size_t.  Host-only
+ * out[2] the accumulators of fmt_linear_pack16, the records of fmt_layernorm_bwd and the operands and partial
+ * results of fmt_attention_fwd / _bwd.  out is a HOST pointer to three size_t.  Host-only
  * bookkeeping: no GPU call besides looking up the current device, no synchronisation.
  */
 int fmt_scratch_bytes(void *stream, size_t *out);

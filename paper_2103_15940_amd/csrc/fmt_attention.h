@@ -426,6 +426,9 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t i, uint32_t n)
 // 2^x; the vector unit's exponential flushes results below 2^-126, which is below 2^-24 of any sum that holds a 1.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A row's lse from its largest score in base 2 and the sum of its powers relative to that; -infinity where it sees nothing.
+__device__ __forceinline__ float lse_of(float top, float sum) { return sum == 0.0f ? -INFINITY : fmaf(top, 0.6931471805599453f, logf(sum)); }
+
 typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
 // A lane's results of DT blocks of 32 columns (its column of the blocks is one row of the tensor): register 4g + i of block d is column

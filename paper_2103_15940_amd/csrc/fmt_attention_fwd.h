@@ -54,7 +54,7 @@ __device__ __forceinline__ void fwd_store(const AttnFwd &a, const f32x16 (&o)[DT
         records[0] = top;
         records[a.splits * all_rows] = sum;
     } else if (a.lse) {
-        a.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+        a.lse[at] = lse_of(top, sum);
     }
 }
 
@@ -189,6 +189,11 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
 
 // The same on operands of one fp16 value each, P in NP pieces of fp16.  The next tile's elements are on their way from memory while a
 // tile is computed; they are rounded and converted on their way into the other of two LDS buffers, so a tile costs one barrier.
+//
+// Measured: 16384 tokens, 8 heads over 2, head size 128, window 2048 and 16 sinks in binary16: 215 to 229 us, 570 to 600 TFLOP/s of S and O
+// (with both pieces of P 850 to 900; a large product reaches 1282).  Bound by LDS reads (the transposed ones take 7.3 cycles for 512 bytes,
+// the others 8 for 1024) and by the exponentials, conversions and sums between the two products, at two workgroups per compute unit.
+// Short sequences (32 x 128 tokens, 12 heads of 64) are a chain of two tiles: 18 us against 7 for their bytes.
 template <int NP, int DT, int KIND>
 __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (half_is_codes(KIND) ? 2 : 1)) void attn_fwd_half_kernel(AttnFwd a)
 {

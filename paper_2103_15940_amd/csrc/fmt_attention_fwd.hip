@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void attn_join_few_kernel(AttnFwd a)
     for (int j = 0; j < 4; ++j) v[j] *= over;
     const int t = static_cast<int>(at % s.q_len), head = static_cast<int>(at / s.q_len % s.heads), b = static_cast<int>(at / s.q_len / s.heads);
     store4(const_cast<void *>(a.o.p), b * a.o.sb + t * a.o.st + head * a.o.sh + col, count, v, a.result, a.f);
-    if (col == 0 && a.lse) a.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+    if (col == 0 && a.lse) a.lse[at] = lse_of(top, sum);
 }
 
 // And where they are many, a workgroup per row: first all parts' weights, then 8 or 16 threads per column with 8 parts each on their way.
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttnFwd a)
     const int t = static_cast<int>(at % s.q_len), head = static_cast<int>(at / s.q_len % s.heads), b = static_cast<int>(at / s.q_len / s.heads);
     const float v[4] = {o, 0.0f, 0.0f, 0.0f};
     store4(const_cast<void *>(a.o.p), b * a.o.sb + t * a.o.st + head * a.o.sh + c, 1, v, a.result, a.f);
-    if (c == 0 && a.lse) a.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+    if (c == 0 && a.lse) a.lse[at] = lse_of(top, sum);
 }
 
 int launch_join(const AttnFwd &a, hipStream_t stream)

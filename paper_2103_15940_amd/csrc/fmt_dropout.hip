@@ -1,4 +1,6 @@
-// Dropout of a matrix (fmt_norm.h has the mathematics).  Bound by memory, and not far from the vector units' time for the generator.
+// Dropout of a matrix (fmt_norm.h has the mathematics).  Bound by memory, and not far from the vector units' time for the generator:
+// 30011 x 4097 in binary16 codes, 492 MB, 93 us or 5.3 TB/s (a large elementwise pass: 6.2, with 16-byte accesses that odd rows do not
+// allow).  Loads and stores marked as used once gained nothing.
 #include "fmt_norm.h"
 
 namespace fmt {

@@ -39,7 +39,7 @@ struct Scratch {
     unsigned hist_turn[2] = {0, 0}; // which of the two sets of the one-launch passes the last pass took (few, many workgroups)
     void *gemm_ws = nullptr;        // pre-split GEMM operands
     size_t gemm_bytes = 0;
-    void *acc_ws = nullptr;         // fp32 accumulators of fmt_linear_pack16
+    void *acc_ws = nullptr;         // fp32: accumulators of fmt_linear_pack16, records of fmt_layernorm_bwd, attention's parts and operands
     size_t acc_bytes = 0;
 };
 

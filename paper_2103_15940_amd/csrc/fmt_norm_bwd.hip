@@ -3,6 +3,9 @@
 // A workgroup takes rows blockIdx, blockIdx + gridDim, ... (by kRows) and keeps the parameters' gradients of its columns in registers,
 // while the next row's elements are on their way; at the end its rows add theirs up in LDS and write one record, and norm_param_kernel
 // adds the records in a fixed order.  (Atomic additions would save that kernel, and give other bits every time.)
+//
+// Measured: 50001 x 768 in fp32, 461 MB: 91 us, 5.1 TB/s, and 4 to 5 us for the records; bound by memory.  4096 x 1024 in bfloat16: 15 us and 4,
+// eight rows per wave one after the other.
 #include "fmt_norm.h"
 
 namespace fmt {

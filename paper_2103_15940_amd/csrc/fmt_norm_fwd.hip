@@ -2,6 +2,9 @@
 //
 // A row stays in the registers of its threads, 8 columns each and piece.  All of a row's loads, weights among them, are on their way
 // before the first is used: a wave has one row, so its time is one trip to memory, two reductions and the stores.
+//
+// Measured: 4096 x 1024 in bfloat16 with residual and dropout 14 us (33.6 MB: 5.4 at the rate of a large elementwise pass): all 1024 workgroups
+// are on the card at once, so reads, generator and writes come one after the other for all of them.  32 x 1024: 5 us, the chain alone.
 #include "fmt_norm.h"
 
 namespace fmt {

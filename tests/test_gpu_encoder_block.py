@@ -74,5 +74,5 @@ def test_training_lowers_the_loss(example):
         losses.append(float((y - target).square().mean()))
         _, grads = block.backward((y - target) * (2.0 / y.numel()) * 1024.0, kept, f)
         for name, grad in grads.items():
-            block.weights[name] -= 20.0 / 1024.0 * grad
+            block.weights[name] -= 4.0 / 1024.0 * grad            # 20 diverges in 64 bits too
     assert losses[-1] < 0.98 * losses[0], losses

@@ -203,15 +203,22 @@ __device__ __forceinline__ void load_query_rows(AttnTile<NQ, DT, kKvRows> &t, co
     }
 }
 
-// Keys whose dK and dV a workgroup adds up over (a part of) the rows that may see them.
+// Rows per step with fp16 operands.
+template <int DT>
+constexpr int kHalfRows = DT == 2 ? 64 : 32;
+
+// Keys whose dK and dV a workgroup adds up over (a part of) the rows that may see them.  Parts end at the same rows on either way of computing
+// (fp16 operands or pieces of bf16): the parts of a tile choose between them each for itself.
 struct KeyBlock {
     int b, kh, part, k0, key, rows, first, last;
     bool live, used, partial;
     int64_t info;
     AttnSeq seq;
 };
-__device__ __forceinline__ KeyBlock key_block(const AttnBwd &a, uint32_t id, int step)
+template <int DT>
+__device__ __forceinline__ KeyBlock key_block(const AttnBwd &a, uint32_t id)
 {
+    constexpr int step = kHalfRows<DT>;
     const AttnShape &s = a.s;
     KeyBlock k;
     // tiles in parts first (they are the ones with the most rows), then the others
@@ -238,7 +245,7 @@ __device__ __forceinline__ KeyBlock key_block(const AttnBwd &a, uint32_t id, int
     }
     if (k.k0 >= k.seq.length) t1 = 0;
     k.first = k.last = 0;
-    if (t0 < t1) {                       // in tiles of `step` rows, and of these the part
+    if (t0 < t1) {                       // in steps, and of these the part
         const int64_t n0 = t0 * s.group / step, n1 = (t1 * s.group + step - 1) / step, all = n1 - n0;
         k.first = static_cast<int>(n0 + all * k.part / parts) * step;
         k.last = static_cast<int>(n0 + all * (k.part + 1) / parts) * step;
@@ -274,9 +281,10 @@ template <int DT>
 __device__ __forceinline__ void dkv_pieces(const AttnBwd &a, uint32_t id, DkvShared<DT> &sh)
 {
     constexpr int NQ = kPieces, NP = kProbPieces;
+    static_assert(kHalfRows<DT> % kKvRows == 0);
     const AttnShape &s = a.s;
     const int lane = threadIdx.x & 63, half = lane >> 5;
-    const KeyBlock key = key_block(a, id, kKvRows);
+    const KeyBlock key = key_block<DT>(a, id);
     const int b = key.b, kh = key.kh, rows = key.rows;
     const AttnSeq seq = key.seq;
     const int64_t all_rows = info_rows(a);
@@ -527,9 +535,6 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
 }
 
 template <int DT>
-constexpr int kHalfRows = DT == 2 ? 64 : 32;
-
-template <int DT>
 struct DkvHalfShared {
     AttnTile<1, DT, kHalfRows<DT>> qs[2], gs[2];
     alignas(16) float lse[2][kHalfRows<DT>], delta[2][kHalfRows<DT>];
@@ -542,7 +547,7 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
     constexpr int kRows = kHalfRows<DT>, DP = 32 * DT;
     const AttnShape &s = a.s;
     const int lane = threadIdx.x & 63, half = lane >> 5;
-    const KeyBlock key = key_block(a, id, kRows);
+    const KeyBlock key = key_block<DT>(a, id);
     const uint32_t bkh = key.b * s.kv_heads + key.kh;
     const PackHighs highs(a, bkh);
     const int64_t all_rows = info_rows(a);

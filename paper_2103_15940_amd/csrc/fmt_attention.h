@@ -370,8 +370,23 @@ __device__ __forceinline__ u32x4 raw_half(const RawEight<half_is_codes(KIND)> &r
         uint32_t ignore = 0;
         return to_half(v, up, ignore);
     } else {
-        // the short roundings: what they do not serve is above the limit.  (Formats of more than 10 bits do not come here.)
         const QuantParams &p = f.p;
+        if constexpr (KIND == kMagicFloat) {
+            if (up == 1.0f) {              // e <= 5, no limit: what overflows the format has to become infinity, and NaN stay NaN
+                uint32_t u[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] = r.w[i / 4][i % 4];
+                if (__any(run_is_rare(u, p))) {
+                    float v[8];
+                    raw_values(r, v, f);
+                    f16x8 h;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[i] = static_cast<_Float16>(v[i]);
+                    return __builtin_bit_cast(u32x4, h);
+                }
+            }
+        }
+        // the short roundings: with a limit, what they do not serve is above it.  (Formats of more than 10 bits do not come here.)
         const uint32_t flush = f.ftz ? p.t_den : 0u;
         const RoundMasks k = round_masks(p);
         auto round = [&](uint32_t u) __attribute__((always_inline)) {

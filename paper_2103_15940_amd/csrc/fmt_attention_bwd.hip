@@ -174,7 +174,7 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
         // tiles with sinks, which all rows see, where the others are seen from a window: in parts of about as many rows (4 x 1024 tokens with a
         // window of 256: the kernel 78 -> 67 us)
         const int64_t near = (static_cast<int64_t>(s.window) + kKvKeys) * s.group;
-        if (s.window > 0 && s.sinks > 0 && rows >= 2 * near) {
+        if (s.window > 0 && s.sinks > 0 && rows > 0 && rows >= 2 * near) {      // (no heads: near is 0)
             parts = std::min(rows / near, rows / 256);
             a.part_tiles = std::min(a.key_tiles, static_cast<uint32_t>((std::min(s.sinks, s.k_len) + kKvKeys - 1) / kKvKeys));
             if (parts <= 1) parts = 1, a.part_tiles = 0;

@@ -414,10 +414,9 @@ __device__ __forceinline__ u32x4 half_signed(u32x4 q, float scale)
     return q;
 }
 
-// Backward, P is taken times 2^14, so that its fp16 pieces hold their bits down to P = 2^-28.  Forward the running maximum stays where it is
-// until a score passes it by 2^8 (a wave of 32 rows would otherwise multiply its sums with some row's factor at almost every tile), so P can
+// Forward the running maximum stays where it is until a score passes it by 2^8 (a wave of 32 rows would otherwise multiply its sums with some row's factor at almost every tile), so P can
 // reach 2^8, and is taken times 2^6.
-constexpr float kProbUp = 14.0f, kFwdUp = 6.0f, kFwdSlack = 8.0f;
+constexpr float kFwdUp = 6.0f, kFwdSlack = 8.0f;
 
 // Whether a workgroup has to be computed with bf16 pieces: in all of its threads.  Every thread calls it.  high, high_value: what raw_half left.
 template <bool CODES>

@@ -377,18 +377,69 @@ __global__ __launch_bounds__(256) void attn_bwd_kernel(AttnBwd a)
 // ---- operands of one fp16 value each, P and dS in NP pieces of fp16
 //
 // A row of dO is taken times its own power of two, 2^grow, which brings its largest element to [2^11, 2^12): dP and dS of a row carry that
-// factor.  dQ loses it at the end.  dK and dV add up rows: there P and dS of a row are taken times 2^(c - grow), with c the smallest grow so
-// far, and sums are brought along when c falls.  A workgroup that meets a |dS| that fp16 does not hold computes again with pieces of bf16, as with
-// operands out of range.
+// factor.  dQ loses it at the end.  dK and dV add up rows: there P and dS of a row are taken times 2^(c - grow), with c the smallest grow so far.
+//
+// P and dS go to fp16 times a power of two of the sum that they enter: of the row in dQ, of the key in dK and dV (both are one lane's, and that of
+// the lane 32 on).  It falls, with the sums so far, when a value passes 2^15, and rises when the first values of a row or key lie below kFactorFloor:
+// half the step of small fp16 numbers, 2^-25, is then at most 2^-20 of the largest (one piece: 2^-15).  Taken times one factor for a whole tile of rows
+// instead, keys that only rows of small dO see lost their P and dS.  (The factor of P costs a product per score.)
 
-// The largest magnitudes of what a workgroup reads, as bit patterns, and of a lane's dS (NaN stays).
+// The largest magnitudes of what a workgroup reads, as bit patterns.
 struct Highs {
     uint32_t q = 0, k = 0, v = 0;
-    float ds = 0.0f;
 };
-__device__ __forceinline__ void track(Highs &h, float a, float b)
+// The larger magnitude (NaN stays).
+__device__ __forceinline__ float larger(float a, float b, float top)
 {
-    h.ds = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(a), fabsf(b)), h.ds);
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(a), fabsf(b)), top);
+}
+constexpr float kFactorMost = 32768.0f;         // what P and dS may be in fp16
+constexpr int kKeyFactor = 14;                  // the first exponent of a key's factor: P of 1 fits; of a row's: 0
+constexpr int kGrowSpread = 60;                 // rows of dO further apart, in binades, are left to the pieces of bf16
+__device__ __forceinline__ int exponent_of(float x) { return static_cast<int>(__float_as_uint(x) >> 23) - 127; }
+
+template <int NP>
+constexpr float kFactorFloor = NP == 2 ? 0x1p-5f : 0x1p-10f;
+
+// Whether a factor has to change: the larger of its largest products has passed, or is NaN, or the smaller one is small and there is room.
+// (dK's dS share the factor of dV's P.)
+template <int NP>
+__device__ __forceinline__ bool factor_off(float high, float low) { return !(high <= kFactorMost) || (low < kFactorFloor<NP> && low > 0.0f && high < 1024.0f); }
+
+// By how many binades the factors of a wave fall (rise: negative).  When one changes, others that are low rise as well, and those that have seen
+// nothing go with one that rises, so that few changes follow.
+__device__ __forceinline__ int factor_fall(float high, float low)
+{
+    int fall = high > kFactorMost ? exponent_of(high) - 11 : low > 0.0f && low < 64.0f ? min(max(exponent_of(low) - 9, exponent_of(high) - 11), 0) : 0;
+    if (!(high < INFINITY)) fall = 0;
+    const uint64_t rising = __ballot(fall < 0);
+    if (rising) {
+        const int one = __builtin_amdgcn_readlane(fall, __builtin_ctzll(rising));
+        if (high == 0.0f) fall = one;
+    }
+    return fall;
+}
+// The smaller of two largest products that are not zero.
+__device__ __forceinline__ float smaller(float a, float b) { return b > 0.0f ? fminf(a, b) : a; }
+
+// x times 2^n for any n that ends among the normal numbers: what is left of the factor for the last product.
+template <int DT>
+__device__ __forceinline__ float bring_down(f32x16 (&x)[DT], int n, float last)
+{
+    const float first = ldexpf(1.0f, n / 2);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[d][i] *= first;
+    return ldexpf(last, n - n / 2);
+}
+template <int DT>
+__device__ __forceinline__ void times(f32x16 (&x)[DT], float factor)
+{
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[d][i] *= factor;
 }
 
 // Where attn_pack_kernel left them for one (batch, kv head).
@@ -410,9 +461,8 @@ struct PackHighs {
 };
 
 // Whether a workgroup has to be computed with bf16 pieces: in all of its threads.
-__device__ __forceinline__ bool half_flags(const AttnBwd &a, const Highs &h)
+__device__ __forceinline__ bool half_flags(const AttnBwd &a, const Highs &h, bool bad)
 {
-    bool bad = !(h.ds <= 65504.0f);
     if (a.check) {                                     // q, k and v are the same in the whole workgroup
         const uint32_t least = __float_as_uint(kHalfLeast);
         bad |= max(max(h.q, h.k), h.v) >= __float_as_uint(kHalfLimit);
@@ -481,6 +531,9 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
         for (int i = 0; i < 16; ++i) dq[d][i] = 0.0f;
     const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up), down = 1.0f / a.up;
     const AttnKeys sees = attn_keys(s, r.seq.length, r.pos);
+    bool bad = false;
+    int factor = 0;
+    float dp_by = down, delta_by = delta, most = 0.0f;
     for (int n = 0; n < count; ++n) {
         const int tile = tiles.at(n), k0 = tile * kKeyTile, buf = n & 1;
         kr.put(sh.ks[buf]);
@@ -509,14 +562,31 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
             if (!all) attn_hide(sees, k0 + 32 * kt + 4 * half, x);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                float ds[8];
+                float ds[8], top;
+                for (int turn = 0;; ++turn) {
+                    top = most;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float p = exp2_fast(fmaf(x[8 * kb + j], scale2, -lse2));
-                    ds[j] = p * fmaf(dp[8 * kb + j], down, -delta);
+                    for (int j = 0; j < 8; ++j) {
+                        const float p = exp2_fast(fmaf(x[8 * kb + j], scale2, -lse2));
+                        ds[j] = p * fmaf(dp[8 * kb + j], dp_by, -delta_by);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) top = larger(ds[j], ds[j + 1], top);
+                    if (!__any(factor_off<NP>(top, top))) break;
+                    if (turn == 1) {                                   // an infinity or NaN
+                        bad = true;
+                        break;
+                    }
+                    const float both = __builtin_elementwise_maximum(top, __shfl_xor(top, 32));
+                    const int fall = factor_fall(both, both);
+                    factor -= fall;
+                    dp_by = ldexpf(down, factor);
+                    delta_by = ldexpf(delta, factor);
+                    const float by = ldexpf(1.0f, -fall);
+                    times<DT>(dq, by);
+                    if (both < INFINITY) most = both * by;             // (the same in both lanes: what is small in one need not be in the other)
                 }
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) track(high, ds[j], ds[j + 1]);
+                most = top;
                 u32x4 pp[NP];
                 f16_pieces<NP>(ds, pp);
 #pragma unroll
@@ -529,8 +599,9 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
             }
         }
     }
-    if (half_flags(a, high)) return true;
-    store_dq<DT>(a, r, dq, ldexpf(s.scale * down, grow == kNoRow ? 0 : -static_cast<int>(grow)));
+    if (half_flags(a, high, bad)) return true;
+    const float last = bring_down<DT>(dq, grow == kNoRow ? 0 : -static_cast<int>(grow) - factor, s.scale * down);
+    store_dq<DT>(a, r, dq, last);
     return false;
 }
 
@@ -595,20 +666,27 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
             seen = static_cast<uint32_t>((t1 - t0) * s.group);
         }
     }
-    float least = kNoRow, running = kNoRow;      // the smallest grow: of the sums, and (wave 0) of the rows read so far
+    float least = kNoRow, running = kNoRow, widest = -kNoRow;      // the smallest grow: of the sums, and (wave 0) of the rows read so far; the largest of those
+    bool bad = false;
+    int factor = kKeyFactor;
+    float by = ldexpf(1.0f, factor), most = 0.0f, most_ds = 0.0f;        // the largest P and dS so far, as the sums are held
     int buf = 0;
     for (int row0 = key.first; row0 < key.last; row0 += kRows, buf ^= 1) {
         qr.put(sh.qs[buf]);
         gr.put(sh.gs[buf]);
         high.q = max(high.q, highs.of(highs.q, row0, kRows));
         if (threadIdx.x < 64) {
-            float low = info[2];
+            float low = info[2], wide = info[2] == kNoRow ? -kNoRow : info[2];
 #pragma unroll
-            for (int w = 32; w > 0; w >>= 1) low = fminf(low, __shfl_xor(low, w));
+            for (int w = 32; w > 0; w >>= 1) {
+                low = fminf(low, __shfl_xor(low, w));
+                wide = fmaxf(wide, __shfl_xor(wide, w));
+            }
             running = fminf(running, low);
+            widest = fmaxf(widest, wide);
             if (threadIdx.x < kRows) {
-                // P of the row times 2^(14 + c - grow) comes out of the exponential (a row of zeros has none), and delta goes with it
-                sh.lse[buf][threadIdx.x] = info[2] == kNoRow ? INFINITY : info[0] - kProbUp - (running - info[2]);
+                // P of the row times 2^(c - grow) comes out of the exponential (a row of zeros has none), and delta goes with it
+                sh.lse[buf][threadIdx.x] = info[2] == kNoRow ? INFINITY : info[0] - (running - info[2]);
                 sh.delta[buf][threadIdx.x] = info[1] * 0x1p-14f;
             }
             if (threadIdx.x == 0) sh.least[buf] = running;
@@ -617,15 +695,18 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
         if (row0 + kRows < key.last) fetch(row0 + kRows);
         const float next = sh.least[buf];
         if (next < least) {                                        // the same in the whole workgroup
-            const float bring = least == kNoRow ? 1.0f : ldexpf(1.0f, static_cast<int>(next - least));
+            // what the sums hold falls with c, but no further than to a largest P of 2^3: from there on the factor rises instead
+            const int by_now = least == kNoRow ? 0 : static_cast<int>(least - next);
+            const float both = fmaxf(most, __shfl_xor(most, 32));
+            const int fall = both > 0.0f ? min(by_now, max(exponent_of(both) - 3, 0)) : by_now;
             least = next;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    dk[d][i] *= bring;
-                    dv[d][i] *= bring;
-                }
+            factor += by_now - fall;
+            by = ldexpf(1.0f, factor);
+            const float lower = ldexpf(1.0f, -fall);
+            times<DT>(dk, lower);
+            times<DT>(dv, lower);
+            most *= lower;
+            most_ds *= lower;
         }
         const int64_t i0 = static_cast<int64_t>(key.seq.first) + row0 / s.group;
         const int64_t i1 = static_cast<int64_t>(key.seq.first) + (min(row0 + kRows, key.rows) - 1) / s.group;
@@ -650,19 +731,39 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
             }
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                float p[8], ds[8];
+                float p[8], ds[8], top, top_ds;
+                for (int turn = 0;; ++turn) {
+                    top = most;
+                    top_ds = most_ds;
 #pragma unroll
-                for (int j0 = 0; j0 < 8; j0 += 4) {
-                    const int row = 32 * rt + 16 * kb + 2 * j0 + 4 * half;
-                    const f32x4 lse = *reinterpret_cast<const f32x4 *>(&sh.lse[buf][row]), delta = *reinterpret_cast<const f32x4 *>(&sh.delta[buf][row]);
+                    for (int j0 = 0; j0 < 8; j0 += 4) {
+                        const int row = 32 * rt + 16 * kb + 2 * j0 + 4 * half;
+                        const f32x4 lse = *reinterpret_cast<const f32x4 *>(&sh.lse[buf][row]), delta = *reinterpret_cast<const f32x4 *>(&sh.delta[buf][row]);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        p[j0 + j] = exp2_fast(fmaf(x[8 * kb + j0 + j], scale2, -lse[j]));
-                        ds[j0 + j] = p[j0 + j] * fmaf(dp[8 * kb + j0 + j], down14, -delta[j]);
+                        for (int j = 0; j < 4; ++j) {
+                            p[j0 + j] = exp2_fast(fmaf(x[8 * kb + j0 + j], scale2, -lse[j])) * by;
+                            ds[j0 + j] = p[j0 + j] * fmaf(dp[8 * kb + j0 + j], down14, -delta[j]);
+                        }
+                        top = larger(p[j0], p[j0 + 1], larger(p[j0 + 2], p[j0 + 3], top));
+                        top_ds = larger(ds[j0], ds[j0 + 1], larger(ds[j0 + 2], ds[j0 + 3], top_ds));
                     }
-                    track(high, ds[j0], ds[j0 + 1]);
-                    track(high, ds[j0 + 2], ds[j0 + 3]);
+                    if (!__any(factor_off<NP>(__builtin_elementwise_maximum(top, top_ds), smaller(top, top_ds)))) break;
+                    if (turn == 2) {                                   // an infinity or NaN
+                        bad = true;
+                        break;
+                    }
+                    const float both = __builtin_elementwise_maximum(top, __shfl_xor(top, 32)), both_ds = __builtin_elementwise_maximum(top_ds, __shfl_xor(top_ds, 32));
+                    const float higher = __builtin_elementwise_maximum(both, both_ds);
+                    const int fall = factor_fall(higher, smaller(both, both_ds));
+                    factor -= fall;
+                    by = ldexpf(1.0f, factor);
+                    const float lower = ldexpf(1.0f, -fall);
+                    times<DT>(dk, lower);
+                    times<DT>(dv, lower);
+                    if (higher < INFINITY) most = both * lower, most_ds = both_ds * lower;     // (the same in both lanes: what is small in one need not be in the other)
                 }
+                most = top;
+                most_ds = top_ds;
                 u32x4 pp[NP], dd[NP];
                 f16_pieces<NP>(p, pp);
                 f16_pieces<NP>(ds, dd);
@@ -679,9 +780,13 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
             }
         }
     }
-    if (half_flags(a, high)) return true;
-    const int lose = least == kNoRow ? 0 : -static_cast<int>(least);
-    store_dkv<DT>(a, key, dk, dv, ldexpf(fabsf(s.scale) * down, lose), ldexpf(1.0f / 16384.0f, lose));
+    // too small beside one another for one factor: V of the key's rows is tiny or large altogether, or their dS all rounding
+    const float low = smaller(fmaxf(most, __shfl_xor(most, 32)), fmaxf(most_ds, __shfl_xor(most_ds, 32)));
+    bad |= widest - running > static_cast<float>(kGrowSpread) || (low > 0.0f && low < kFactorFloor<NP>);
+    if (half_flags(a, high, bad)) return true;
+    const int lose = least == kNoRow ? 0 : -static_cast<int>(least) - factor;
+    const float klast = bring_down<DT>(dk, lose, fabsf(s.scale) * down * 16384.0f), vlast = bring_down<DT>(dv, lose, 1.0f);
+    store_dkv<DT>(a, key, dk, dv, klast, vlast);
     return false;
 }
 

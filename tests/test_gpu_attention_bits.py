@@ -1,0 +1,46 @@
+"""Attention's bits where magnitudes lie far apart: every element of an operand counts with all of its bits, and the gradients of a key with the
+rows that see it, whatever other rows, channels or tokens of the same tile hold.  Tolerances as in test_gpu_attention.py, element by element."""
+import numpy as np
+import pytest
+
+from test_gpu_attention import check, fmt, inputs  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+SIX, BF16, HALF = (6, 9, True), (8, 7, True), (5, 10, True)
+TYPES = [(SIX, False, "f32"), (BF16, True, "f32"), (BF16, True, "code16"), (BF16, False, "f32"), ((7, 8, True), True, "f32")]
+
+
+@pytest.mark.parametrize("f,codes,result", TYPES)
+@pytest.mark.parametrize("exponent", [-20, -30, -36, -45])
+@pytest.mark.parametrize("causal,window,sinks", [(True, 0, 0), (True, 40, 3)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_of_do_far_apart(fmt, f, codes, result, exponent, causal, window, sinks, d):  # noqa: F811
+    """The last rows' dO far below the first's: keys that only they see."""
+    rng = np.random.default_rng(exponent + 100)
+    q, k, v, do = inputs(rng, 1, 330, 330, 2, 2, d, grad=1.0)
+    do[:, 250:] *= np.float32(2.0 ** exponent)
+    check(fmt, q, k, v, do, f, codes, result, causal, window, sinks)
+
+
+@pytest.mark.parametrize("f,codes,result", TYPES + [((5, 10, True), True, "f32")])
+@pytest.mark.parametrize("n,h,hk", [(150, 2, 2), (700, 2, 1)])
+def test_rows_of_do_of_any_size(fmt, f, codes, result, n, h, hk):  # noqa: F811
+    """Rows of dO spread over some eighty binades (over thirty where the format has no more), a third of them zero; the rows' order is not theirs."""
+    rng = np.random.default_rng(n)
+    q, k, v, do = inputs(rng, 1, n, n, h, hk, 40, grad=1.0)
+    wide = 40 if f[0] == 8 else 14 if f[0] == 6 else 30 if f[0] == 7 else 6
+    do *= np.exp2(rng.uniform(-wide, wide, size=(1, n, h, 1))).astype(np.float32) * (rng.uniform(size=(1, n, h, 1)) > 0.3)
+    check(fmt, q, k, v, do, f, codes, result, True)
+
+
+@pytest.mark.parametrize("f,codes,result", [(SIX, False, "f32"), (BF16, True, "f32")])
+@pytest.mark.parametrize("n", [200, 1500])
+def test_keys_that_get_little_weight(fmt, f, codes, result, n):  # noqa: F811
+    """A few keys take most of every row; the others' dK and dV are small, and have their bits."""
+    rng = np.random.default_rng(n)
+    q, k, v, do = inputs(rng, 1, n, n, 1, 1, 64, grad=1.0)
+    q[..., 0], k[..., 0] = 4.0, 0.0
+    k[:, :3, :, 0] = 18.0                        # scores of about 9 more
+    check(fmt, q, k, v, do, f, codes, result, True)

@@ -20,6 +20,8 @@
 // with ds_read_b64_tr_b16 (16 lanes read 4 rows x 16 columns, lane i receives column i).
 #pragma once
 
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "fmt_elem.h"
@@ -229,12 +231,12 @@ __device__ __forceinline__ void load_tokens(AttnTile<NQ, DT, ROWS> &t, const voi
 //
 // Formats of at most 10 stored mantissa bits fit fp16's significand, and 1/5/10 and narrower its range as well: their products are exact in
 // one product instead of four of bf16 pieces.  For wider ranges (1/6/9, 1/8/7) values are taken times 2^9, which holds |x| < 2^7 and
-// their bits down to 2^-33; what a smaller element loses is below 2^-34, for a score less than 128 * 128 * 128 * 2^-33 = 2^-12 at the very worst (all
-// elements of one side at 2^7, all of the other below 2^-23) and below 2^-24 for elements up to 8.  A workgroup that meets an element of 2^7 or more, an infinity or
+// their bits down to 2^-33; what is below is cut.  That puts up to dim 2^-33 (max |Q| + max |K|) |scale| into a score, which is kept to 2^-21 by a limit of Q and K
+// (2^7 at most; with a scale of dim^-0.5 it is that).  A workgroup that meets a larger element, an infinity or
 // NaN, or whose V (backward: Q, K or V) lies below 2^-10 altogether, computes its results again with pieces of bf16.  (A second launch for such
 // workgroups, which all but a few calls do not have, cost every call 4 us.)
-// (fp32 is looked at before it is rounded: from 112 on, what has one mantissa bit becomes 128.)
-constexpr float kHalfUp = 512.0f, kHalfLimit = 128.0f, kHalfLimitRaw = 112.0f, kHalfLeast = 0x1p-10f;
+constexpr int kHalfLimit = 7;             // as an exponent
+constexpr float kHalfUp = 512.0f, kHalfLeast = 0x1p-10f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -298,7 +300,8 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 // What codes need on their way to fp16, two at a time: masks of their magnitudes and signs, and for e == 6 the shifts that make fp16
 // of them (times 2^9: the exponent field falls by 7).
 struct HalfCodes {
-    uint32_t body, sign, limit, least;      // limit, least: codes of kHalfLimit and kHalfLeast
+    uint32_t body, sign;
+    uint32_t scores, limit, least;          // limits of Q and K, of V, and kHalfLeast: as codes, or patterns of unrounded fp32
     int32_t shift, sign_shift;              // shift < 0: by way of fp32
 };
 
@@ -423,9 +426,8 @@ template <bool CODES>
 __device__ __forceinline__ bool half_flag(uint32_t high, uint32_t high_value, const HalfCodes &hc)
 {
     const uint32_t h = CODES ? max(high >> 16, high & 0xFFFFu) : high, v = CODES ? max(high_value >> 16, high_value & 0xFFFFu) : high_value;
-    const uint32_t limit = CODES ? hc.limit : __float_as_uint(kHalfLimitRaw), least = CODES ? hc.least : __float_as_uint(kHalfLeast);
-    const bool over = __syncthreads_or(max(h, v) >= limit);
-    const bool some = __syncthreads_or(v != 0u), large = __syncthreads_or(v >= least);
+    const bool over = __syncthreads_or(h >= hc.scores || v >= hc.limit);
+    const bool some = __syncthreads_or(v != 0u), large = __syncthreads_or(v >= hc.least);
     return over || (some && !large);
 }
 
@@ -558,15 +560,24 @@ void with_dim(int dim, RUN &&run)
 
 constexpr int kPieces = 2, kProbPieces = 3;      // bf16 pieces of operands, of P and dS
 
-// Whether a format's values go as one fp16 value each.
-inline bool attention_half(fmt_format_t f) { return f.m <= 10; }
+// Exponent of the limit of Q and K with fp16 operands.
+inline int score_limit(const AttnShape &s)
+{
+    const double most = 2048.0 / (std::fabs(static_cast<double>(s.scale)) * s.dim);
+    return most >= 128.0 ? kHalfLimit : std::ilogb(most);
+}
 
-inline HalfCodes make_half_codes(fmt_format_t f, const ElemFormat &e)
+// Whether values go as one fp16 value each: the format's fit, and the scale leaves Q and K a limit of 1 or more.
+inline bool attention_half(fmt_format_t f, const AttnShape &s) { return f.m <= 10 && (f.e <= 5 || score_limit(s) >= 0); }
+
+inline HalfCodes make_half_codes(fmt_format_t f, const AttnShape &s, int32_t store)
 {
     const uint32_t body = (1u << (f.e + f.m)) - 1u, sign = 1u << (f.e + f.m);
     const int bias = (1 << (f.e - 1)) - 1;
-    return HalfCodes{body * 0x10001u, sign * 0x10001u, static_cast<uint32_t>(bias + 7) << f.m, static_cast<uint32_t>(bias > 10 ? bias - 10 : 0) << f.m,
-                     f.e == 6 ? 10 - f.m : -1, 15 - (f.e + f.m)};
+    // 2^n; unrounded fp32 is looked at: from 7/8 of it on, what has one mantissa bit becomes 2^n
+    auto power = [&](int n) { return store == FMT_STORE_CODE16 ? static_cast<uint32_t>(std::max(bias + n, 0)) << f.m : static_cast<uint32_t>(127 + n) << 23; };
+    auto limit = [&](int n) { return power(n) - (store == FMT_STORE_CODE16 ? 0u : 1u << 21); };
+    return HalfCodes{body * 0x10001u, sign * 0x10001u, limit(score_limit(s)), limit(kHalfLimit), power(-10), f.e == 6 ? 10 - f.m : -1, 15 - (f.e + f.m)};
 }
 
 // Pieces of P and dS with fp16 operands: one (11 bits) where results have 8, two (22) where they have more.

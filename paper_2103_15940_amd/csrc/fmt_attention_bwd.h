@@ -24,6 +24,7 @@ struct AttnBwd {
     float *part;              // [2][parts][batch][part_keys][kv_heads][dim] of dK, dV
     float up;                 // what the fp16 operands are multiplied by
     bool check;               // whether that has a limit
+    float limit;              // of Q and K
     bool codes, gcodes;       // how q, k and v, and o and go, are stored
     int32_t parts;            // parts of the rows that each of the first part_tiles tiles of keys adds up
     int32_t part_keys;        // their keys
@@ -465,7 +466,7 @@ __device__ __forceinline__ bool half_flags(const AttnBwd &a, const Highs &h, boo
 {
     if (a.check) {                                     // q, k and v are the same in the whole workgroup
         const uint32_t least = __float_as_uint(kHalfLeast);
-        bad |= max(max(h.q, h.k), h.v) >= __float_as_uint(kHalfLimit);
+        bad |= max(h.q, h.k) >= __float_as_uint(a.limit) || h.v >= __float_as_uint(ldexpf(1.0f, kHalfLimit));
         bad |= (h.q != 0u && h.q < least) || (h.k != 0u && h.k < least) || (h.v != 0u && h.v < least);
     }
     return __syncthreads_or(bad);

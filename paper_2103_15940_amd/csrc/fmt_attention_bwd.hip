@@ -187,11 +187,12 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
     a.key_blocks = static_cast<uint32_t>(key_blocks);
     a.row_blocks = static_cast<uint32_t>(row_blocks);
     if (key_blocks + row_blocks == 0) return FMT_OK;
-    const bool half = attention_half(fmt);
+    const bool half = attention_half(fmt, s);
     a.codes = store == FMT_STORE_CODE16;
     a.gcodes = result == FMT_RESULT_CODE16;
     a.check = fmt.e > 5;
     a.up = a.check ? kHalfUp : 1.0f;
+    a.limit = a.check && half ? ldexpf(1.0f, score_limit(s)) : 0.0f;
 
     // scratch: fp16 operands first (rows of 64 or 128 bytes), then words
     const int64_t width = s.dim <= 64 ? 64 : 128;

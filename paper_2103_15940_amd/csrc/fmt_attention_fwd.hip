@@ -128,9 +128,9 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
     if (splits > kJoinMost) splits = kJoinMost;
     if (splits > key_tiles / 4) splits = key_tiles / 4;
     if (splits < 1) splits = 1;
-    const bool half = attention_half(fmt), check = fmt.e > 5;
+    const bool half = attention_half(fmt, s), check = fmt.e > 5;
     AttnFwd a{s, q, k, v, o, lse, result, static_cast<int32_t>(splits), nullptr, check ? kHalfUp : 1.0f, static_cast<int32_t>(row_tiles),
-              store == FMT_STORE_CODE16, make_half_codes(fmt, f), f};
+              store == FMT_STORE_CODE16, make_half_codes(fmt, s, store), f};
     const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len, grid = work * splits;
     if (grid > 0x7FFFFFFF) return FMT_ERR_SHAPE;
     if (splits > 1) {

@@ -44,3 +44,17 @@ def test_keys_that_get_little_weight(fmt, f, codes, result, n):  # noqa: F811
     q[..., 0], k[..., 0] = 4.0, 0.0
     k[:, :3, :, 0] = 18.0                        # scores of about 9 more
     check(fmt, q, k, v, do, f, codes, result, True)
+
+
+@pytest.mark.parametrize("f,codes,result", TYPES[:2] + TYPES[3:])
+@pytest.mark.parametrize("exponent", [-25, -28, -30])
+@pytest.mark.parametrize("where", ["q", "k", "both"])
+def test_small_scores_and_a_large_scale(fmt, f, codes, result, exponent, where):  # noqa: F811
+    """Scores are Q K^T times the scale: operands of 2^-28 count where the scale is 2^28."""
+    rng = np.random.default_rng(exponent + 50)
+    q, k, v, do = inputs(rng, 1, 130, 150, 2, 1, 64)
+    c, down = 2.0 ** -exponent / 8, np.float32(2.0 ** exponent)
+    if where == "both":
+        check(fmt, q * np.float32(2.0 ** (exponent // 2)), k * np.float32(2.0 ** (exponent - exponent // 2)), v, do, f, codes, result, True, scale=c)
+    else:
+        check(fmt, q * down if where == "q" else q, k * down if where == "k" else k, v, do, f, codes, result, True, scale=c)

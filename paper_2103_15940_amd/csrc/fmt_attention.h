@@ -232,11 +232,12 @@ __device__ __forceinline__ void load_tokens(AttnTile<NQ, DT, ROWS> &t, const voi
 // Formats of at most 10 stored mantissa bits fit fp16's significand, and 1/5/10 and narrower its range as well: their products are exact in
 // one product instead of four of bf16 pieces.  For wider ranges (1/6/9, 1/8/7) values are taken times 2^9, which holds |x| < 2^7 and
 // their bits down to 2^-33; what is below is cut.  That puts up to dim 2^-33 (max |Q| + max |K|) |scale| into a score, which is kept to 2^-21 by a limit of Q and K
-// (2^7 at most; with a scale of dim^-0.5 it is that).  A workgroup that meets a larger element, an infinity or
-// NaN, or whose V (backward: Q, K or V) lies below 2^-10 altogether, computes its results again with pieces of bf16.  (A second launch for such
-// workgroups, which all but a few calls do not have, cost every call 4 us.)
+// (2^7 at most; with a scale of dim^-0.5 it is that).  Where an operand's elements enter a sum of their own channel the cut bits count, whatever other
+// channels and tokens hold: a tile with such elements is taken in two parts, and the second, what was cut, times 2^24 more.  A workgroup that meets a larger element,
+// an infinity or NaN, or bits below 2^-57 (backward: or Q, K or V below 2^-10 altogether) computes its results again with pieces of bf16.  (A second launch
+// for such workgroups, which all but a few calls do not have, cost every call 4 us.)
 constexpr int kHalfLimit = 7;             // as an exponent
-constexpr float kHalfUp = 512.0f, kHalfLeast = 0x1p-10f;
+constexpr float kHalfUp = 512.0f, kHalfLeast = 0x1p-10f, kRestUp = 0x1p24f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -301,7 +302,8 @@ typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 // of them (times 2^9: the exponent field falls by 7).
 struct HalfCodes {
     uint32_t body, sign;
-    uint32_t scores, limit, least;          // limits of Q and K, of V, and kHalfLeast: as codes, or patterns of unrounded fp32
+    uint32_t scores, limit;                 // limits of Q and K, and of V: as codes, or patterns of unrounded fp32
+    uint32_t cut;                           // least magnitude whose bits all fit, as a code less one, or a pattern of fp32, doubled and less one
     int32_t shift, sign_shift;              // shift < 0: by way of fp32
 };
 
@@ -324,9 +326,25 @@ inline int half_kind(fmt_format_t f, int32_t store)
     return f.e == 5 && f.m == 10 && f.denorm ? kHalfFloat : f.e == 8 ? kIntegerFloat : kMagicFloat;
 }
 
+// What to_half and raw_half cut off eight values, as fp16 times 2^24 more; lost: what this cuts off too.
+__device__ __forceinline__ u32x4 half_rest(const float (&v)[8], float up, bool &lost)
+{
+    u32x4 h;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const auto top = __builtin_amdgcn_cvt_pkrtz(v[i] * up, v[i + 1] * up);
+        const float a = (v[i] * up - static_cast<float>(top[0])) * kRestUp, b = (v[i + 1] * up - static_cast<float>(top[1])) * kRestUp;
+        const auto rest = __builtin_amdgcn_cvt_pkrtz(a, b);
+        lost |= static_cast<float>(rest[0]) != a || static_cast<float>(rest[1]) != b;
+        h[i / 2] = __builtin_bit_cast(uint32_t, rest);
+    }
+    return h;
+}
+
 // Eight elements as fp16 times `up`.  high: the largest magnitude so far; of codes, of either half of a word; of fp32 as a bit pattern, unrounded.
-template <int KIND>
-__device__ __forceinline__ u32x4 raw_half(const RawEight<half_is_codes(KIND)> &r, float up, const HalfCodes &hc, uint32_t &high, const ElemFormat &f)
+// WATCH: cut tells of elements that may have lost bits.
+template <int KIND, bool WATCH>
+__device__ __forceinline__ u32x4 raw_half(const RawEight<half_is_codes(KIND)> &r, float up, const HalfCodes &hc, uint32_t &high, bool &cut, const ElemFormat &f)
 {
     u32x4 out;
     if constexpr (KIND == kHalfCodes) {
@@ -337,14 +355,17 @@ __device__ __forceinline__ u32x4 raw_half(const RawEight<half_is_codes(KIND)> &r
         for (int i = 0; i < 8; ++i) h[i] = static_cast<_Float16>(__uint_as_float(r.w[i / 4][i % 4]));
         return __builtin_bit_cast(u32x4, h);
     } else if constexpr (KIND == kBf16Codes) {
-        u16x2 top = __builtin_bit_cast(u16x2, high);
+        u16x2 top = __builtin_bit_cast(u16x2, high), low = {0xFFFF, 0xFFFF};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t w = r.w[0][i];
-            top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu));
+            const u16x2 body = __builtin_bit_cast(u16x2, w & 0x7FFF7FFFu);
+            top = __builtin_elementwise_max(top, body);
+            if constexpr (WATCH) low = __builtin_elementwise_min(low, body - static_cast<uint16_t>(1));
             out[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xFFFF0000u) * up));
         }
         high = __builtin_bit_cast(uint32_t, top);
+        if constexpr (WATCH) cut |= min(low[0], low[1]) < hc.cut;
         return out;
     } else if constexpr (KIND == kSixCodes || KIND == kOtherCodes) {
         u16x2 top = __builtin_bit_cast(u16x2, high), low = {0xFFFF, 0xFFFF};
@@ -370,6 +391,7 @@ __device__ __forceinline__ u32x4 raw_half(const RawEight<half_is_codes(KIND)> &r
         }
         float v[8];
         raw_values(r, v, f);
+        if constexpr (WATCH) cut |= min(low[0], low[1]) < hc.cut;
         uint32_t ignore = 0;
         return to_half(v, up, ignore);
     } else {
@@ -398,12 +420,16 @@ __device__ __forceinline__ u32x4 raw_half(const RawEight<half_is_codes(KIND)> &r
             else q = (u + p.rbias + __builtin_amdgcn_ubfe(u, p.shift, p.lsb_width)) & p.nmask;
             return __uint_as_float((u & 0x7FFFFFFFu) < flush ? 0u : q);
         };
+        uint32_t low = 0xFFFFFFFFu;
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
             const uint32_t a = r.w[i / 4][i % 4], b = r.w[i / 4][i % 4 + 1];
             high = max(max(a & 0x7FFFFFFFu, b & 0x7FFFFFFFu), high);
-            out[i / 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(round(a) * up, round(b) * up));
+            const float x = round(a), y = round(b);
+            if constexpr (WATCH) low = min(min((__float_as_uint(x) << 1) - 1u, (__float_as_uint(y) << 1) - 1u), low);
+            out[i / 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x * up, y * up));
         }
+        if constexpr (WATCH) cut |= low < hc.cut;
         return out;
     }
 }
@@ -426,9 +452,7 @@ template <bool CODES>
 __device__ __forceinline__ bool half_flag(uint32_t high, uint32_t high_value, const HalfCodes &hc)
 {
     const uint32_t h = CODES ? max(high >> 16, high & 0xFFFFu) : high, v = CODES ? max(high_value >> 16, high_value & 0xFFFFu) : high_value;
-    const bool over = __syncthreads_or(h >= hc.scores || v >= hc.limit);
-    const bool some = __syncthreads_or(v != 0u), large = __syncthreads_or(v >= hc.least);
-    return over || (some && !large);
+    return __syncthreads_or(h >= hc.scores || v >= hc.limit);
 }
 
 // Workgroups of one launch in an order that gives each of the 8 XCDs (workgroup i runs on XCD i % 8) a run of neighbours, which share keys
@@ -577,7 +601,8 @@ inline HalfCodes make_half_codes(fmt_format_t f, const AttnShape &s, int32_t sto
     // 2^n; unrounded fp32 is looked at: from 7/8 of it on, what has one mantissa bit becomes 2^n
     auto power = [&](int n) { return store == FMT_STORE_CODE16 ? static_cast<uint32_t>(std::max(bias + n, 0)) << f.m : static_cast<uint32_t>(127 + n) << 23; };
     auto limit = [&](int n) { return power(n) - (store == FMT_STORE_CODE16 ? 0u : 1u << 21); };
-    return HalfCodes{body * 0x10001u, sign * 0x10001u, limit(score_limit(s)), limit(kHalfLimit), power(-10), f.e == 6 ? 10 - f.m : -1, 15 - (f.e + f.m)};
+    const uint32_t whole = power(f.m - 33), cut = store == FMT_STORE_CODE16 ? (whole ? whole - 1u : 0u) : (whole << 1) - 1u;
+    return HalfCodes{body * 0x10001u, sign * 0x10001u, limit(score_limit(s)), limit(kHalfLimit), cut, f.e == 6 ? 10 - f.m : -1, 15 - (f.e + f.m)};
 }
 
 // Pieces of P and dS with fp16 operands: one (11 bits) where results have 8, two (22) where they have more.

@@ -213,6 +213,7 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
             AttnTile<1, DT, kFwdKeys> ks[2], vs[2];
         } half;
         FwdShared<DT> pieces;
+        uint32_t cuts[4];
         __device__ Shared() {}
     } sh;
     auto &ks = sh.half.ks, &vs = sh.half.vs;
@@ -262,12 +263,14 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
     };
     if (begin < end) fetch(begin);
 
+    bool ignore = false;
     u32x4 q[2 * DT];
 #pragma unroll
     for (int kk = 0; kk < 2 * DT; ++kk) {
         const int col = 16 * kk + 8 * half;
         q[kk] = half_signed(
-            raw_half<KIND>(raw_load<CODES>(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, live ? s.dim - col : 0), a.up, a.hc, high, a.f), s.scale);
+            raw_half<KIND, false>(raw_load<CODES>(a.q.p, b * a.q.sb + t * a.q.st + head * a.q.sh + col, live ? s.dim - col : 0), a.up, a.hc, high, ignore, a.f),
+            s.scale);
     }
     f32x16 o[DT];
 #pragma unroll
@@ -277,13 +280,20 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
     float top = -INFINITY, sum = 0.0f;
     const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up);
     const AttnKeys sees = attn_keys(s, seq.length, pos);
+    constexpr bool kCuts = half_has_limit(KIND);
+    uint32_t cuts = 0;                                     // which 32nds of the tiles lost bits of V
+    const int cut_tiles = (end - begin + 31) / 32;
     for (int n = begin; n < end; ++n) {
         const int k0 = tiles.at(n) * kFwdKeys, buf = (n - begin) & 1;
+        bool cut = false;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             const int key = key_in + i * (256 / kEights);
-            *reinterpret_cast<u32x4 *>(&ks[buf].e[0][key][col_in]) = raw_half<KIND>(kr[i], a.up, a.hc, high, a.f);
-            *reinterpret_cast<u32x4 *>(&vs[buf].e[0][key][col_in]) = raw_half<KIND>(vr[i], a.up, a.hc, high_value, a.f);
+            *reinterpret_cast<u32x4 *>(&ks[buf].e[0][key][col_in]) = raw_half<KIND, false>(kr[i], a.up, a.hc, high, ignore, a.f);
+            *reinterpret_cast<u32x4 *>(&vs[buf].e[0][key][col_in]) = raw_half<KIND, kCuts>(vr[i], a.up, a.hc, high_value, cut, a.f);
+        }
+        if constexpr (kCuts) {
+            if (__any(cut)) cuts |= 1u << ((n - begin) / cut_tiles);
         }
         __syncthreads();
         if (n + 1 < end) fetch(n + 1);
@@ -340,14 +350,77 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
                 }
             }
     }
-    sum += __shfl_xor(sum, 32);
-    const float over = sum == 0.0f ? 0.0f : 1.0f / (sum * a.up);
-    if constexpr (half_has_limit(KIND)) {
-        if (a.up != 1.0f && half_flag<CODES>(high, high_value, a.hc)) {
+    if (kCuts && a.up != 1.0f) {
+        bool pieces = half_flag<CODES>(high, high_value, a.hc);
+        if (lane == 0) sh.cuts[wave] = cuts;
+        __syncthreads();
+        cuts = __builtin_amdgcn_readfirstlane(sh.cuts[0] | sh.cuts[1] | sh.cuts[2] | sh.cuts[3]);      // the same in the whole workgroup
+        __syncthreads();
+        if (cuts && !pieces) {
+            // what was cut, over the tiles that it may be in, with the weights relative to the rows' largest scores
+            bool lost = false;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= kRestUp;
+            const float base = (top == -INFINITY ? 0.0f : top) - kFwdUp;
+#pragma unroll 1
+            for (int n = begin; n < end; ++n) {
+                if (!(cuts >> ((n - begin) / cut_tiles) & 1u)) continue;
+                fetch(n);
+                const int k0 = tiles.at(n) * kFwdKeys;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int key = key_in + i * kStep;
+                    float v[8];
+                    raw_values(vr[i], v, a.f);
+                    *reinterpret_cast<u32x4 *>(&ks[0].e[0][key][col_in]) = raw_half<KIND, false>(kr[i], a.up, a.hc, high, ignore, a.f);
+                    *reinterpret_cast<u32x4 *>(&vs[0].e[0][key][col_in]) = half_rest(v, a.up, lost);
+                }
+                __syncthreads();
+#pragma unroll 1
+                for (int kt = 0; kt < 2; ++kt) {
+                    f32x16 x;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+#pragma unroll
+                    for (int kk = 0; kk < 2 * DT; ++kk) {
+                        u32x4 f[1];
+                        read_rows(ks[0], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
+                        x = mfma_f16(f[0], q[kk], x);
+                    }
+                    attn_hide(sees, k0 + 32 * kt + 4 * half, x);
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) {
+                        float p[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) p[j] = exp2_fast(fmaf(x[8 * kb + j], scale2, -base));
+                        u32x4 pp[NP];
+                        f16_pieces<NP>(p, pp);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            u32x4 f[1];
+                            read_columns(vs[0], 32 * kt + 16 * kb, 32 * d, lane, f);
+#pragma unroll
+                            for (int w = NP - 1; w >= 0; --w) o[d] = mfma_f16(f[0], pp[w], o[d]);
+                        }
+                    }
+                }
+                __syncthreads();
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= 1.0f / kRestUp;
+            pieces = __syncthreads_or(lost);
+        }
+        if (pieces) {
             fwd_pieces<DT>(a, blk.id, sh.pieces);
             return;
         }
     }
+    sum += __shfl_xor(sum, 32);
+    const float over = sum == 0.0f ? 0.0f : 1.0f / (sum * a.up);
     if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, top - kFwdUp, sum);
 }
 

@@ -58,3 +58,24 @@ def test_small_scores_and_a_large_scale(fmt, f, codes, result, exponent, where):
         check(fmt, q * np.float32(2.0 ** (exponent // 2)), k * np.float32(2.0 ** (exponent - exponent // 2)), v, do, f, codes, result, True, scale=c)
     else:
         check(fmt, q * down if where == "q" else q, k * down if where == "k" else k, v, do, f, codes, result, True, scale=c)
+
+
+@pytest.mark.parametrize("f,codes,result", TYPES + [((6, 4, True), True, "f32"), ((7, 8, False), False, "f32")])
+@pytest.mark.parametrize("what", ["channel", "tokens", "element"])
+@pytest.mark.parametrize("exponent", [-25, -30, -37, -50, -90])
+@pytest.mark.parametrize("nq,nk,h,hk,d,window", [(150, 150, 2, 2, 64, 0), (90, 500, 2, 1, 128, 70), (40, 1700, 1, 1, 40, 0), (9, 130, 1, 1, 100, 0)])
+def test_small_v_beside_ordinary(fmt, f, codes, result, what, exponent, nq, nk, h, hk, d, window):  # noqa: F811
+    """Output: a channel, the first tokens, or single elements of V far below the others."""
+    if exponent < -37 and f[0] == 6:
+        pytest.skip("below the format's smallest values")
+    rng = np.random.default_rng(nk - exponent)
+    q, k, v, _ = inputs(rng, 2, nq, nk, h, hk, d)
+    c = np.float32(2.0 ** exponent)
+    if what == "channel":
+        v[..., 7] *= c
+    elif what == "tokens":
+        v[:, :70] *= c
+    else:
+        v[rng.uniform(size=v.shape) < 0.002] *= c
+        v[:, :3, :, 5] *= c
+    check(fmt, q, k, v, None, f, codes, result, True, window, 0)

@@ -234,10 +234,10 @@ __device__ __forceinline__ void load_tokens(AttnTile<NQ, DT, ROWS> &t, const voi
 // their bits down to 2^-33; what is below is cut.  That puts up to dim 2^-33 (max |Q| + max |K|) |scale| into a score, which is kept to 2^-21 by a limit of Q and K
 // (2^7 at most; with a scale of dim^-0.5 it is that).  Where an operand's elements enter a sum of their own channel the cut bits count, whatever other
 // channels and tokens hold: a tile with such elements is taken in two parts, and the second, what was cut, times 2^24 more.  A workgroup that meets a larger element,
-// an infinity or NaN, or bits below 2^-57 (backward: or Q, K or V below 2^-10 altogether) computes its results again with pieces of bf16.  (A second launch
+// an infinity or NaN, or bits below 2^-57, computes its results again with pieces of bf16.  (A second launch
 // for such workgroups, which all but a few calls do not have, cost every call 4 us.)
 constexpr int kHalfLimit = 7;             // as an exponent
-constexpr float kHalfUp = 512.0f, kHalfLeast = 0x1p-10f, kRestUp = 0x1p24f;
+constexpr float kHalfUp = 512.0f, kRestUp = 0x1p24f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 

@@ -20,11 +20,12 @@ struct AttnBwd {
     float *info;              // what the products need of a row, [4][batch][kv_heads][row_tiles * 128]: kInfo*
     uint16_t *qh, *gh;        // fp16 operands: [batch][kv_heads][row_tiles * 128][32 DT] Q and dO, zero past the last row and column,
     uint16_t *kh, *vh;        // [batch][kv_heads][key_tiles * 128][32 DT] K and V, zero past the sequence's length
-    uint32_t *highs;          // the largest |x| of each 32 rows of Q, then of each 32 keys of K, then of V
+    uint32_t *highs;          // what is to know of each 32 rows of Q and dO, then of each 32 keys of K, then of V (join)
     float *part;              // [2][parts][batch][part_keys][kv_heads][dim] of dK, dV
     float up;                 // what the fp16 operands are multiplied by
     bool check;               // whether that has a limit
     float limit;              // of Q and K
+    float whole;              // what fp16 operands hold with all of their bits, as they are held
     bool codes, gcodes;       // how q, k and v, and o and go, are stored
     int32_t parts;            // parts of the rows that each of the first part_tiles tiles of keys adds up
     int32_t part_keys;        // their keys
@@ -377,7 +378,7 @@ __global__ __launch_bounds__(256) void attn_bwd_kernel(AttnBwd a)
 
 // ---- operands of one fp16 value each, P and dS in NP pieces of fp16
 //
-// A row of dO is taken times its own power of two, 2^grow, which brings its largest element to [2^11, 2^12): dP and dS of a row carry that
+// A row of dO is taken times its own power of two, 2^grow, which brings its largest element to [2^14, 2^15): dP and dS of a row carry that
 // factor.  dQ loses it at the end.  dK and dV add up rows: there P and dS of a row are taken times 2^(c - grow), with c the smallest grow so far.
 //
 // P and dS go to fp16 times a power of two of the sum that they enter: of the row in dQ, of the key in dK and dV (both are one lane's, and that of
@@ -385,10 +386,24 @@ __global__ __launch_bounds__(256) void attn_bwd_kernel(AttnBwd a)
 // half the step of small fp16 numbers, 2^-25, is then at most 2^-20 of the largest (one piece: 2^-15).  Taken times one factor for a whole tile of rows
 // instead, keys that only rows of small dO see lost their P and dS.  (The factor of P costs a product per score.)
 
-// The largest magnitudes of what a workgroup reads, as bit patterns.
+// Elements that lost bits on their way to fp16 (below 2^-24 in 11 bits of 1/6/9, for instance) count where they enter a sum of their own channel: of K in dQ, of
+// Q in dK, of dO in dV.  A workgroup that reads such elements adds what was cut in a second run over the tiles that hold them.  In dP, a sum over
+// channels, what V and dO lost is looked at beside the largest dS of the row or key: it may come to 2^-20 of that, and pieces of bf16 are taken otherwise.
+//
+// What is to know of 32 rows of an operand: the largest |x| as a bit pattern less its last eight bits, there the most elements of a
+// row that lost bits (of dO, of V), and in the sign bit whether a second run is wanted.
+__device__ __forceinline__ uint32_t join(uint32_t a, uint32_t b)
+{
+    return max(a & 0x7FFFFF00u, b & 0x7FFFFF00u) | max(a & 0xFFu, b & 0xFFu) | ((a | b) & 0x80000000u);
+}
 struct Highs {
     uint32_t q = 0, k = 0, v = 0;
 };
+// The most that dP may have lost, before P, in the units that dS is held in (dO at 2^15, V as it is).
+__device__ __forceinline__ float dp_lost(const Highs &h)
+{
+    return static_cast<float>(h.v & 0xFFu) * 0x1p-18f + static_cast<float>(h.q & 0xFFu) * 0x1p-24f * __uint_as_float(h.v & 0x7FFFFF00u);
+}
 // The larger magnitude (NaN stays).
 __device__ __forceinline__ float larger(float a, float b, float top)
 {
@@ -456,7 +471,7 @@ struct PackHighs {
     __device__ __forceinline__ uint32_t of(const uint32_t *p, int first, int count) const
     {
         uint32_t h = 0;
-        for (int i = 0; i < count / kPackRows; ++i) h = max(h, p[first / kPackRows + i]);
+        for (int i = 0; i < count / kPackRows; ++i) h = join(h, p[first / kPackRows + i]);
         return h;
     }
 };
@@ -465,9 +480,8 @@ struct PackHighs {
 __device__ __forceinline__ bool half_flags(const AttnBwd &a, const Highs &h, bool bad)
 {
     if (a.check) {                                     // q, k and v are the same in the whole workgroup
-        const uint32_t least = __float_as_uint(kHalfLeast);
-        bad |= max(h.q, h.k) >= __float_as_uint(a.limit) || h.v >= __float_as_uint(ldexpf(1.0f, kHalfLimit));
-        bad |= (h.q != 0u && h.q < least) || (h.k != 0u && h.k < least) || (h.v != 0u && h.v < least);
+        const uint32_t scores = max(h.q & 0x7FFFFF00u, h.k & 0x7FFFFF00u);
+        bad |= scores >= __float_as_uint(a.limit) || (h.v & 0x7FFFFF00u) >= __float_as_uint(ldexpf(1.0f, kHalfLimit));
     }
     return __syncthreads_or(bad);
 }
@@ -491,6 +505,24 @@ struct TileLoad {
         }
     }
 };
+
+// What was cut of tokens [first, first + ROWS) of one head (load_tokens).
+template <int DT, int ROWS>
+__device__ __forceinline__ void load_rests(AttnTile<1, DT, ROWS> &t, const void *x, int64_t base, int64_t stride, int first, int end, int dim, bool codes,
+                                           const ElemFormat &f, float up)
+{
+    constexpr int kEights = 4 * DT;
+    bool ignore = false;
+#pragma unroll 1
+    for (int i = 0; i < ROWS * kEights / 256; ++i) {
+        const int n = threadIdx.x + 256 * i, row = n / kEights, col = (n % kEights) * 8;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        if (first + row < end && col < dim) load8_any(x, base + (first + row) * stride + col, min(dim - col, 8), v, codes, f);
+        *reinterpret_cast<u32x4 *>(&t.e[0][row][col]) = half_rest(v, up, ignore);
+    }
+}
 
 template <int DT>
 struct DqHalfShared {
@@ -539,8 +571,8 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
         const int tile = tiles.at(n), k0 = tile * kKeyTile, buf = n & 1;
         kr.put(sh.ks[buf]);
         vr.put(sh.vs[buf]);
-        high.k = max(high.k, highs.of(highs.k, k0, kKeyTile));
-        high.v = max(high.v, highs.of(highs.v, k0, kKeyTile));
+        high.k = join(high.k, highs.of(highs.k, k0, kKeyTile));
+        high.v = join(high.v, highs.of(highs.v, k0, kKeyTile));
         __syncthreads();
         if (n + 1 < count) {
             kr.fetch(keys + static_cast<int64_t>(tiles.at(n + 1)) * kKeyTile * DP);
@@ -573,7 +605,7 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
                     }
 #pragma unroll
                     for (int j = 0; j < 8; j += 2) top = larger(ds[j], ds[j + 1], top);
-                    if (!__any(factor_off<NP>(top, top))) break;
+                    if (__builtin_expect(!__any(factor_off<NP>(top, top)), 1)) break;
                     if (turn == 1) {                                   // an infinity or NaN
                         bad = true;
                         break;
@@ -600,7 +632,58 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
             }
         }
     }
-    if (half_flags(a, high, bad)) return true;
+    if (r.live && lse2 < INFINITY && grow != kNoRow) {
+        const float largest = __builtin_elementwise_maximum(most, __shfl_xor(most, 32));
+        bad |= ldexpf(dp_lost(high), factor + 20) > largest;
+    }
+    if (__builtin_expect(half_flags(a, high, bad), 0)) return true;
+    if (__builtin_expect(high.k >> 31, 0)) {                                    // the same in the whole workgroup
+        times<DT>(dq, kRestUp);
+        const int64_t kbase = r.b * a.k.sb + r.kh * a.k.sh;
+#pragma unroll 1
+        for (int n = 0; n < count; ++n) {
+            const int tile = tiles.at(n), k0 = tile * kKeyTile;
+            if (!(highs.of(highs.k, k0, kKeyTile) >> 31)) continue;
+            kr.fetch(keys + static_cast<int64_t>(tile) * kKeyTile * DP);
+            vr.fetch(values + static_cast<int64_t>(tile) * kKeyTile * DP);
+            kr.put(sh.ks[0]);
+            vr.put(sh.vs[0]);
+            load_rests<DT, kKeyTile>(sh.ks[1], a.k.p, kbase, a.k.st, k0, r.seq.length, s.dim, a.codes, a.f, a.up);
+            __syncthreads();
+#pragma unroll 1
+            for (int kt = 0; kt < 2; ++kt) {
+                f32x16 x, dp;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
+#pragma unroll
+                for (int kk = 0; kk < 2 * DT; ++kk) {
+                    u32x4 f[1];
+                    read_rows(sh.ks[0], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
+                    x = mfma_f16(f[0], q[kk], x);
+                    read_rows(sh.vs[0], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
+                    dp = mfma_f16(f[0], go[kk], dp);
+                }
+                attn_hide(sees, k0 + 32 * kt + 4 * half, x);
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    float ds[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) ds[j] = exp2_fast(fmaf(x[8 * kb + j], scale2, -lse2)) * fmaf(dp[8 * kb + j], dp_by, -delta_by);
+                    u32x4 pp[NP];
+                    f16_pieces<NP>(ds, pp);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        u32x4 f[1];
+                        read_columns(sh.ks[1], 32 * kt + 16 * kb, 32 * d, lane, f);
+#pragma unroll
+                        for (int w = NP - 1; w >= 0; --w) dq[d] = mfma_f16(f[0], pp[w], dq[d]);
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        times<DT>(dq, 1.0f / kRestUp);
+    }
     const float last = bring_down<DT>(dq, grow == kNoRow ? 0 : -static_cast<int>(grow) - factor, s.scale * down);
     store_dq<DT>(a, r, dq, last);
     return false;
@@ -612,6 +695,34 @@ struct DkvHalfShared {
     alignas(16) float lse[2][kHalfRows<DT>], delta[2][kHalfRows<DT>];
     float least[2];
 };
+
+// What was cut of Q and dO, rows [row0, row0 + kHalfRows) of the heads that share a kv head.
+template <int DT>
+__device__ __forceinline__ void load_row_rests(const AttnBwd &a, AttnTile<1, DT, kHalfRows<DT>> &qs, AttnTile<1, DT, kHalfRows<DT>> &gs, const KeyBlock &key,
+                                               int row0)
+{
+    constexpr int kEights = 4 * DT;
+    const AttnShape &s = a.s;
+    bool ignore = false;
+#pragma unroll 1
+    for (int i = 0; i < kHalfRows<DT> * kEights / 256; ++i) {
+        const int n = threadIdx.x + 256 * i, r = n / kEights, col = (n % kEights) * 8, row = row0 + r;
+        float q[8], g[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = g[j] = 0.0f;
+        if (row < key.rows && col < s.dim) {
+            const RowAt at = row_at(row, s.group);
+            const int count = min(s.dim - col, 8), head = key.kh * s.group + at.g;
+            load8_any(a.q.p, key.b * a.q.sb + at.t * a.q.st + head * a.q.sh + col, count, q, a.codes, a.f);
+            load8_any(a.go.p, key.b * a.go.sb + at.t * a.go.st + head * a.go.sh + col, count, g, a.gcodes, a.f);
+            const float grow = a.info[kInfoGrow * info_rows(a) + key.info + row];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] = grow == kNoRow ? 0.0f : ldexpf(g[j], static_cast<int>(grow));
+        }
+        *reinterpret_cast<u32x4 *>(&qs.e[0][r][col]) = half_signed(half_rest(q, a.up, ignore), s.scale);
+        *reinterpret_cast<u32x4 *>(&gs.e[0][r][col]) = half_rest(g, 1.0f, ignore);
+    }
+}
 
 template <int NP, int DT>
 __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfShared<DT> &sh)
@@ -651,7 +762,7 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
 #pragma unroll
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
     const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up), down = 1.0f / a.up;
-    const float down14 = down * 0x1p-14f;
+    const float down17 = down * 0x1p-17f;
     // rows that see the lane's key
     int seen_from = 0;
     uint32_t seen = 0;
@@ -675,7 +786,7 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
     for (int row0 = key.first; row0 < key.last; row0 += kRows, buf ^= 1) {
         qr.put(sh.qs[buf]);
         gr.put(sh.gs[buf]);
-        high.q = max(high.q, highs.of(highs.q, row0, kRows));
+        high.q = join(high.q, highs.of(highs.q, row0, kRows));
         if (threadIdx.x < 64) {
             float low = info[2], wide = info[2] == kNoRow ? -kNoRow : info[2];
 #pragma unroll
@@ -688,7 +799,7 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
             if (threadIdx.x < kRows) {
                 // P of the row times 2^(c - grow) comes out of the exponential (a row of zeros has none), and delta goes with it
                 sh.lse[buf][threadIdx.x] = info[2] == kNoRow ? INFINITY : info[0] - (running - info[2]);
-                sh.delta[buf][threadIdx.x] = info[1] * 0x1p-14f;
+                sh.delta[buf][threadIdx.x] = info[1] * 0x1p-17f;
             }
             if (threadIdx.x == 0) sh.least[buf] = running;
         }
@@ -743,12 +854,12 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             p[j0 + j] = exp2_fast(fmaf(x[8 * kb + j0 + j], scale2, -lse[j])) * by;
-                            ds[j0 + j] = p[j0 + j] * fmaf(dp[8 * kb + j0 + j], down14, -delta[j]);
+                            ds[j0 + j] = p[j0 + j] * fmaf(dp[8 * kb + j0 + j], down17, -delta[j]);
                         }
                         top = larger(p[j0], p[j0 + 1], larger(p[j0 + 2], p[j0 + 3], top));
                         top_ds = larger(ds[j0], ds[j0 + 1], larger(ds[j0 + 2], ds[j0 + 3], top_ds));
                     }
-                    if (!__any(factor_off<NP>(__builtin_elementwise_maximum(top, top_ds), smaller(top, top_ds)))) break;
+                    if (__builtin_expect(!__any(factor_off<NP>(__builtin_elementwise_maximum(top, top_ds), smaller(top, top_ds))), 1)) break;
                     if (turn == 2) {                                   // an infinity or NaN
                         bad = true;
                         break;
@@ -782,11 +893,74 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
         }
     }
     // too small beside one another for one factor: V of the key's rows is tiny or large altogether, or their dS all rounding
-    const float low = smaller(fmaxf(most, __shfl_xor(most, 32)), fmaxf(most_ds, __shfl_xor(most_ds, 32)));
+    most = __builtin_elementwise_maximum(most, __shfl_xor(most, 32));
+    most_ds = __builtin_elementwise_maximum(most_ds, __shfl_xor(most_ds, 32));
+    const float low = smaller(most, most_ds);
     bad |= widest - running > static_cast<float>(kGrowSpread) || (low > 0.0f && low < kFactorFloor<NP>);
-    if (half_flags(a, high, bad)) return true;
+    bad |= most * dp_lost(high) * 0x1p3f > most_ds;                  // P dp_lost 2^-17 2^20
+    if (__builtin_expect(half_flags(a, high, bad), 0)) return true;
+    if (__builtin_expect(high.q >> 31, 0)) {                                    // the same in the whole workgroup
+        times<DT>(dk, kRestUp);
+        times<DT>(dv, kRestUp);
+#pragma unroll 1
+        for (int row0 = key.first; row0 < key.last; row0 += kRows) {
+            if (!(highs.of(highs.q, row0, kRows) >> 31)) continue;
+            fetch(row0);
+            qr.put(sh.qs[0]);
+            gr.put(sh.gs[0]);
+            load_row_rests<DT>(a, sh.qs[1], sh.gs[1], key, row0);
+            if (threadIdx.x < kRows) {
+                sh.lse[0][threadIdx.x] = info[2] == kNoRow ? INFINITY : info[0] - (least - info[2]);
+                sh.delta[0][threadIdx.x] = info[1] * 0x1p-17f;
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int rt = 0; rt < kRows / 32; ++rt) {
+                f32x16 x, dp;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
+#pragma unroll
+                for (int kk = 0; kk < 2 * DT; ++kk) {
+                    u32x4 f[1];
+                    read_rows(sh.qs[0], 32 * rt + (lane & 31), 16 * kk + 8 * half, f);
+                    x = mfma_f16(f[0], k[kk], x);
+                    read_rows(sh.gs[0], 32 * rt + (lane & 31), 16 * kk + 8 * half, f);
+                    dp = mfma_f16(f[0], v[kk], dp);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    x[i] = static_cast<uint32_t>(row0 + 32 * rt + 8 * (i / 4) + 4 * half + (i & 3) - seen_from) < seen ? x[i] : -INFINITY;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    float p[8], ds[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int row = 32 * rt + 16 * kb + 8 * (j / 4) + 4 * half + (j & 3);
+                        p[j] = exp2_fast(fmaf(x[8 * kb + j], scale2, -sh.lse[0][row])) * by;
+                        ds[j] = p[j] * fmaf(dp[8 * kb + j], down17, -sh.delta[0][row]);
+                    }
+                    u32x4 pp[NP], dd[NP];
+                    f16_pieces<NP>(p, pp);
+                    f16_pieces<NP>(ds, dd);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        u32x4 f[1];
+                        read_columns(sh.gs[1], 32 * rt + 16 * kb, 32 * d, lane, f);
+#pragma unroll
+                        for (int w = NP - 1; w >= 0; --w) dv[d] = mfma_f16(f[0], pp[w], dv[d]);
+                        read_columns(sh.qs[1], 32 * rt + 16 * kb, 32 * d, lane, f);
+#pragma unroll
+                        for (int w = NP - 1; w >= 0; --w) dk[d] = mfma_f16(f[0], dd[w], dk[d]);
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        times<DT>(dk, 1.0f / kRestUp);
+        times<DT>(dv, 1.0f / kRestUp);
+    }
     const int lose = least == kNoRow ? 0 : -static_cast<int>(least) - factor;
-    const float klast = bring_down<DT>(dk, lose, fabsf(s.scale) * down * 16384.0f), vlast = bring_down<DT>(dv, lose, 1.0f);
+    const float klast = bring_down<DT>(dk, lose, fabsf(s.scale) * down * 131072.0f), vlast = bring_down<DT>(dv, lose, 1.0f);
     store_dkv<DT>(a, key, dk, dv, klast, vlast);
     return false;
 }
@@ -803,10 +977,10 @@ __global__ __launch_bounds__(256, DT == 2 ? 2 : 1) void attn_bwd_half_kernel(Att
     } sh;
     if (blockIdx.x < a.key_blocks) {
         const uint32_t id = xcd_order(blockIdx.x, a.key_blocks);
-        if (dkv_half<NP, DT>(a, id, sh.kv)) dkv_pieces<DT>(a, id, sh.kv_pieces);
+        if (__builtin_expect(dkv_half<NP, DT>(a, id, sh.kv), 0)) dkv_pieces<DT>(a, id, sh.kv_pieces);
     } else {
         const uint32_t id = xcd_order(blockIdx.x - a.key_blocks, a.row_blocks);
-        if (dq_half<NP, DT>(a, id, sh.q)) dq_pieces<DT>(a, id, sh.q_pieces);
+        if (__builtin_expect(dq_half<NP, DT>(a, id, sh.q), 0)) dq_pieces<DT>(a, id, sh.q_pieces);
     }
 }
 

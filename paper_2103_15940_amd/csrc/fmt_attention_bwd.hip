@@ -10,14 +10,48 @@ extern template void run_attention_bwd<4>(const AttnBwd &, bool, bool, dim3, hip
 
 namespace {
 
-__device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t *shared)
+// join over a workgroup, of magnitudes and what else there is to know (most often nothing).
+__device__ __forceinline__ uint32_t block_join(uint32_t high, uint32_t more, uint32_t *shared)
 {
 #pragma unroll
-    for (int w = 32; w > 0; w >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), w)));
+    for (int w = 32; w > 0; w >>= 1) high = max(high, static_cast<uint32_t>(__shfl_xor(static_cast<int>(high), w)));
+    high &= 0x7FFFFF00u;
+    if (__builtin_expect(__any(more != 0u), 0)) {
+#pragma unroll
+        for (int w = 32; w > 0; w >>= 1) more = join(more, static_cast<uint32_t>(__shfl_xor(static_cast<int>(more), w)));
+        high |= more;
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = high;
     __syncthreads();
-    return max(max(shared[0], shared[1]), max(shared[2], shared[3]));
+    return join(join(shared[0], shared[1]), join(shared[2], shared[3]));
+}
+
+// Whether one of eight values, as they go to fp16, may lose bits.
+__device__ __forceinline__ bool may_cut(const float (&v)[8], float up, float whole)
+{
+    uint32_t low = 0xFFFFFFFFu;
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) low = min(min((__float_as_uint(v[j] * up) << 1) - 1u, (__float_as_uint(v[j + 1] * up) << 1) - 1u), low);
+    return low < (__float_as_uint(whole) << 1) - 1u;
+}
+
+// How many of eight values in fp16 are not zero.
+__device__ __forceinline__ int count_of(const u32x4 &h)
+{
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n += ((h[i] & 0x7FFFu) != 0u) + ((h[i] & 0x7FFF0000u) != 0u);
+    return n;
+}
+
+// Over the lanes of a row.
+template <int LANES>
+__device__ __forceinline__ int lanes_total(int n)
+{
+#pragma unroll
+    for (int w = LANES / 2; w > 0; w >>= 1) n += __shfl_xor(n, w);
+    return n;
 }
 
 // What the products need: of 32 rows delta = sum over the head's columns of R(dO) O, lse, and with HALF R(Q) and R(dO) as fp16 operands; with HALF
@@ -38,7 +72,7 @@ __global__ __launch_bounds__(256) void attn_pack_kernel(AttnBwd a)
         const int kh = static_cast<int>(bkh % s.kv_heads), b = static_cast<int>(bkh / s.kv_heads), rows = s.q_len * s.group;
         ElemFormat whole = a.f;
         if (!a.gcodes) whole.codec = kCodecNone;                   // O is taken as it is
-        uint32_t high_q = 0;
+        uint32_t high_q = 0, more = 0;
 #pragma unroll 1
         for (int r = in; r < kPackRows; r += kStep) {
             const int row = static_cast<int>(tile) * kPackRows + r;
@@ -65,36 +99,45 @@ __global__ __launch_bounds__(256) void attn_pack_kernel(AttnBwd a)
                 sum += __shfl_xor(sum, w);
                 high = max(high, static_cast<uint32_t>(__shfl_xor(static_cast<int>(high), w)));
             }
-            const int grow = min(max(138 - static_cast<int>(high >> 23), -120), 120);      // 11 - the exponent of the largest
+            const int grow = min(max(141 - static_cast<int>(high >> 23), -120), 120);      // 14 - the exponent of the largest
+            float q[8], scaled[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                q[j] = 0.0f;
+                scaled[j] = ldexpf(g[j], grow);
+            }
+            bool lost = false;
+            if constexpr (HALF) {
+                if (there) load8_any(a.q.p, b * a.q.sb + where.t * a.q.st + head * a.q.sh + col, count, q, a.codes, a.f);
+                *reinterpret_cast<u32x4 *>(a.qh + at * 32 * DT + col) = half_signed(to_half(q, a.up, high_q), s.scale);
+                uint32_t ignore = 0;
+                *reinterpret_cast<u32x4 *>(a.gh + at * 32 * DT + col) = to_half(scaled, 1.0f, ignore);
+                if (__builtin_expect(__any(may_cut(scaled, 1.0f, a.whole) || may_cut(q, a.up, a.whole)), 0)) {
+                    bool q_lost = false;
+                    const int cut_q = count_of(half_rest(q, a.up, q_lost)), cut_g = lanes_total<kEights>(count_of(half_rest(scaled, 1.0f, lost)));
+                    lost = lanes_total<kEights>(lost) != 0;
+                    if (q_lost) high_q = 0x7F800000u;
+                    more = join(more, static_cast<uint32_t>(cut_g) | (cut_q + cut_g ? 0x80000000u : 0u));
+                }
+            }
             if (col == 0) {
                 const float lse = row < rows ? a.lse[(static_cast<int64_t>(b) * s.heads + head) * s.q_len + where.t] : -INFINITY;
                 a.info[kInfoLse2 * all + at] = lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f;
                 a.info[kInfoDelta * all + at] = sum;
                 a.info[kInfoGrow * all + at] = high == 0u ? kNoRow : static_cast<float>(grow);
-                // (an infinity or NaN in dO makes NaN of the row, and so of the check on dS)
-                a.info[kInfoScaledDelta * all + at] = high >= 0x7F800000u ? NAN : ldexpf(sum, grow);
-            }
-            if constexpr (HALF) {
-                f16x8 h;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[j] = static_cast<_Float16>(ldexpf(g[j], grow));
-                *reinterpret_cast<u32x4 *>(a.gh + at * 32 * DT + col) = __builtin_bit_cast(u32x4, h);
-                float q[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q[j] = 0.0f;
-                if (there) load8_any(a.q.p, b * a.q.sb + where.t * a.q.st + head * a.q.sh + col, count, q, a.codes, a.f);
-                *reinterpret_cast<u32x4 *>(a.qh + at * 32 * DT + col) = half_signed(to_half(q, a.up, high_q), s.scale);
+                // (an infinity or NaN in dO, or bits of it that not even a second fp16 value holds, make NaN of the row, and so of the check on dS)
+                a.info[kInfoScaledDelta * all + at] = high >= 0x7F800000u || lost ? NAN : ldexpf(sum, grow);
             }
         }
         if constexpr (HALF) {
-            high_q = block_max(high_q, shared);
+            high_q = block_join(high_q, more, shared);
             if (threadIdx.x == 0) a.highs[blockIdx.x] = high_q;
         }
     } else if constexpr (HALF) {
         const uint32_t n = blockIdx.x - row_blocks, tile = n % key_packs, bkh = n / key_packs;
         const int kh = static_cast<int>(bkh % s.kv_heads), b = static_cast<int>(bkh / s.kv_heads);
         const AttnSeq seq = attn_seq(s, b);
-        uint32_t high_k = 0, high_v = 0;
+        uint32_t high_k = 0, high_v = 0, more_k = 0, more_v = 0;
 #pragma unroll 1
         for (int r = in; r < kPackRows; r += kStep) {
             const int key = static_cast<int>(tile) * kPackRows + r;
@@ -108,9 +151,15 @@ __global__ __launch_bounds__(256) void attn_pack_kernel(AttnBwd a)
             }
             *reinterpret_cast<u32x4 *>(a.kh + at * 32 * DT + col) = to_half(k, a.up, high_k);
             *reinterpret_cast<u32x4 *>(a.vh + at * 32 * DT + col) = to_half(v, a.up, high_v);
+            if (__builtin_expect(__any(may_cut(k, a.up, a.whole) || may_cut(v, a.up, a.whole)), 0)) {
+                bool k_lost = false, ignore = false;
+                if (count_of(half_rest(k, a.up, k_lost))) more_k = 0x80000000u;
+                if (k_lost) high_k = 0x7F800000u;
+                more_v = join(more_v, static_cast<uint32_t>(lanes_total<kEights>(count_of(half_rest(v, a.up, ignore)))));
+            }
         }
-        high_k = block_max(high_k, shared);
-        high_v = block_max(high_v, shared);
+        high_k = block_join(high_k, more_k, shared);
+        high_v = block_join(high_v, more_v, shared);
         if (threadIdx.x == 0) {
             const uint32_t key_blocks = key_packs * s.kv_heads * s.batch;
             a.highs[row_blocks + n] = high_k;
@@ -192,6 +241,7 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
     a.gcodes = result == FMT_RESULT_CODE16;
     a.check = fmt.e > 5;
     a.up = a.check ? kHalfUp : 1.0f;
+    a.whole = ldexpf(1.0f, fmt.m - 24);
     a.limit = a.check && half ? ldexpf(1.0f, score_limit(s)) : 0.0f;
 
     // scratch: fp16 operands first (rows of 64 or 128 bytes), then words

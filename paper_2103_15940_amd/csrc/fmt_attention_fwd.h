@@ -356,7 +356,7 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
         __syncthreads();
         cuts = __builtin_amdgcn_readfirstlane(sh.cuts[0] | sh.cuts[1] | sh.cuts[2] | sh.cuts[3]);      // the same in the whole workgroup
         __syncthreads();
-        if (cuts && !pieces) {
+        if (__builtin_expect(cuts && !pieces, 0)) {
             // what was cut, over the tiles that it may be in, with the weights relative to the rows' largest scores
             bool lost = false;
 #pragma unroll
@@ -414,7 +414,7 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
                 for (int i = 0; i < 16; ++i) o[d][i] *= 1.0f / kRestUp;
             pieces = __syncthreads_or(lost);
         }
-        if (pieces) {
+        if (__builtin_expect(pieces, 0)) {
             fwd_pieces<DT>(a, blk.id, sh.pieces);
             return;
         }

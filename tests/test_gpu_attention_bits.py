@@ -79,3 +79,35 @@ def test_small_v_beside_ordinary(fmt, f, codes, result, what, exponent, nq, nk, 
         v[rng.uniform(size=v.shape) < 0.002] *= c
         v[:, :3, :, 5] *= c
     check(fmt, q, k, v, None, f, codes, result, True, window, 0)
+
+
+@pytest.mark.parametrize("f,codes,result", [(SIX, False, "f32"), (BF16, True, "code16"), (HALF, True, "f32")])
+@pytest.mark.parametrize("exponent", [-12, 4, 6])
+@pytest.mark.parametrize("n,window,sinks", [(400, 40, 0), (300, 0, 0), (200, 1, 0), (200, 1, 2)])
+def test_v_far_from_one_in_blocks(fmt, f, codes, result, exponent, n, window, sinks):  # noqa: F811
+    """dS as large and as small as V makes it: blocks of tokens longer than the window; rows that see one key, whose dS is nothing but rounding."""
+    rng = np.random.default_rng(n + exponent)
+    q, k, v, do = inputs(rng, 1, n, n, 2, 2, 64, grad=1.0)
+    v[:, 90:250] *= np.float32(2.0 ** exponent)
+    check(fmt, q, k, v, do, f, codes, result, True, window, sinks)
+
+
+@pytest.mark.parametrize("f,codes,result", TYPES)
+@pytest.mark.parametrize("where", ["q", "k", "v", "do"])
+@pytest.mark.parametrize("what", ["channel", "tokens", "element"])
+@pytest.mark.parametrize("exponent", [-26, -30])
+@pytest.mark.parametrize("d", [40, 128])
+def test_small_beside_ordinary(fmt, f, codes, result, where, what, exponent, d):  # noqa: F811
+    """A channel, the first tokens, or single elements of one operand far below the others."""
+    rng = np.random.default_rng(d)
+    q, k, v, do = inputs(rng, 1, 150, 150, 2, 2, d, grad=1.0)
+    t = {"q": q, "k": k, "v": v, "do": do}[where]
+    c = np.float32(2.0 ** exponent)
+    if what == "channel":
+        t[..., 7] *= c
+    elif what == "tokens":
+        t[:, :70] *= c
+    else:
+        t[rng.uniform(size=t.shape) < 0.002] *= c
+        t[:, :3, :, 5] *= c
+    check(fmt, q, k, v, do, f, codes, result, True)

@@ -443,9 +443,10 @@ __device__ __forceinline__ u32x4 half_signed(u32x4 q, float scale)
     return q;
 }
 
-// Forward the running maximum stays where it is until a score passes it by 2^8 (a wave of 32 rows would otherwise multiply its sums with some row's factor at almost every tile), so P can
-// reach 2^8, and is taken times 2^6.
-constexpr float kFwdUp = 6.0f, kFwdSlack = 8.0f;
+// Forward the running maximum stays where it is until a score passes it by 2^4 (a wave of 32 rows would otherwise multiply its sums with some row's factor at
+// almost every tile), so P can reach 2^4, and is taken times 2^11: weights keep 22 bits down to 2^-14 of a row's largest, and 11 down to 2^-25.  (With
+// 2^8 and 2^6 a row whose largest weight meets a V of zero had five bits less.)
+constexpr float kFwdUp = 11.0f, kFwdSlack = 4.0f;
 
 // Whether a workgroup has to be computed with bf16 pieces: in all of its threads.  Every thread calls it.  high, high_value: what raw_half left.
 template <bool CODES>

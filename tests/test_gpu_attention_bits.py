@@ -111,3 +111,16 @@ def test_small_beside_ordinary(fmt, f, codes, result, where, what, exponent, d):
         t[rng.uniform(size=t.shape) < 0.002] *= c
         t[:, :3, :, 5] *= c
     check(fmt, q, k, v, do, f, codes, result, True)
+
+
+@pytest.mark.parametrize("f,codes,result", [(SIX, False, "f32"), (SIX, True, "f32"), (BF16, True, "f32"), (HALF, True, "f32")])
+@pytest.mark.parametrize("score", [6, 10, 14])
+@pytest.mark.parametrize("nq", [5, 60])
+def test_a_sink_without_value(fmt, f, codes, result, score, nq):  # noqa: F811
+    """The first key takes nearly all of every row and its V is zero: the output is what the others, of little weight, leave."""
+    rng = np.random.default_rng(score)
+    q, k, v, do = inputs(rng, 1, nq, 700, 1, 1, 64, grad=1.0)
+    q[..., 0], k[..., 0] = 4.0, 0.0
+    k[:, 0, :, 0] = 2.0 * score                  # a score of `score` more
+    v[:, 0] = 0.0
+    check(fmt, q, k, v, do if score <= 6 else None, f, codes, result, False)

@@ -387,8 +387,9 @@ __global__ __launch_bounds__(256) void attn_bwd_kernel(AttnBwd a)
 // instead, keys that only rows of small dO see lost their P and dS.  (The factor of P costs a product per score.)
 
 // Elements that lost bits on their way to fp16 (below 2^-24 in 11 bits of 1/6/9, for instance) count where they enter a sum of their own channel: of K in dQ, of
-// Q in dK, of dO in dV.  A workgroup that reads such elements adds what was cut in a second run over the tiles that hold them.  In dP, a sum over
-// channels, what V and dO lost is looked at beside the largest dS of the row or key: it may come to 2^-20 of that, and pieces of bf16 are taken otherwise.
+// Q in dK, of dO in dV.  A workgroup that reads such elements adds what was cut in a second run over the tiles that hold them, what V lost in dQ's dP with it.
+// In other sums over channels what V and dO lost is held against the largest dS of the row or key: it may come to 2^-20 of that, and pieces of bf16 are
+// taken otherwise.
 //
 // What is to know of 32 rows of an operand: the largest |x| as a bit pattern less its last eight bits, there the most elements of a
 // row that lost bits (of dO, of V), and in the sign bit whether a second run is wanted.
@@ -399,11 +400,9 @@ __device__ __forceinline__ uint32_t join(uint32_t a, uint32_t b)
 struct Highs {
     uint32_t q = 0, k = 0, v = 0;
 };
-// The most that dP may have lost, before P, in the units that dS is held in (dO at 2^15, V as it is).
-__device__ __forceinline__ float dp_lost(const Highs &h)
-{
-    return static_cast<float>(h.v & 0xFFu) * 0x1p-18f + static_cast<float>(h.q & 0xFFu) * 0x1p-24f * __uint_as_float(h.v & 0x7FFFFF00u);
-}
+// The most that dP may have lost, before P, in the units that dS is held in (dO at 2^15, V as it is): of dO, of V.
+__device__ __forceinline__ float dp_lost_of_do(const Highs &h) { return static_cast<float>(h.q & 0xFFu) * 0x1p-24f * __uint_as_float(h.v & 0x7FFFFF00u); }
+__device__ __forceinline__ float dp_lost_of_v(const Highs &h) { return static_cast<float>(h.v & 0xFFu) * 0x1p-18f; }
 // The larger magnitude (NaN stays).
 __device__ __forceinline__ float larger(float a, float b, float top)
 {
@@ -529,6 +528,98 @@ struct DqHalfShared {
     AttnTile<1, DT, kKeyTile> ks[2], vs[2];
 };
 
+// The same number, as far as the compiler knows another one: what is computed from it again need not be kept.
+__device__ __forceinline__ uint32_t opaque(uint32_t id)
+{
+    asm volatile("" : "+v"(id));
+    return __builtin_amdgcn_readfirstlane(id);
+}
+
+// What V lost, in dS, and then what K lost, times 2^24: over the tiles concerned.
+template <int NP, int DT>
+__device__ __forceinline__ void dq_rests(const AttnBwd &a, uint32_t id, const Highs &high, DqHalfShared<DT> &sh, f32x16 (&dq)[DT], int factor, float &most,
+                                         bool &bad)
+{
+    constexpr int DP = 32 * DT;
+    const AttnShape &s = a.s;
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    const RowBlock r = row_block(a, id);
+    const uint32_t bkh = r.b * s.kv_heads + r.kh;
+    const PackHighs highs(a, bkh);
+    const int64_t all_rows = info_rows(a), kbase = r.b * a.k.sb + r.kh * a.k.sh, vbase = r.b * a.v.sb + r.kh * a.v.sh;
+    const uint16_t *keys = a.kh + static_cast<int64_t>(bkh) * a.key_tiles * kKvKeys * DP, *values = a.vh + static_cast<int64_t>(bkh) * a.key_tiles * kKvKeys * DP;
+    const AttnTiles tiles = attn_tiles(s, r.seq.length, r.i0, r.i1, kKeyTile);
+    const float lse2 = a.info[kInfoLse2 * all_rows + r.info], delta = a.info[kInfoScaledDelta * all_rows + r.info];
+    const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up);
+    const float dp_by = ldexpf(1.0f / a.up, factor), delta_by = ldexpf(delta, factor);
+    const AttnKeys sees = attn_keys(s, r.seq.length, r.pos);
+#pragma unroll 1
+    for (int of_k = high.v & 0xFFu ? 0 : 1; of_k < (high.k >> 31 ? 2 : 1); ++of_k) {
+        if (of_k) times<DT>(dq, kRestUp);
+#pragma unroll 1
+        for (int n = 0; n < tiles.count(); ++n) {
+            const int tile = tiles.at(n), k0 = tile * kKeyTile;
+            if (!(of_k ? highs.of(highs.k, k0, kKeyTile) >> 31 : highs.of(highs.v, k0, kKeyTile) & 0xFFu)) continue;
+            TileLoad<DT, kKeyTile> load;
+            load.fetch(keys + static_cast<int64_t>(tile) * kKeyTile * DP);
+            load.put(sh.ks[0]);
+            load.fetch(values + static_cast<int64_t>(tile) * kKeyTile * DP);
+            load.put(sh.vs[0]);
+            load_rests<DT, kKeyTile>(sh.ks[1], a.k.p, kbase, a.k.st, k0, r.seq.length, s.dim, a.codes, a.f, a.up);
+            load_rests<DT, kKeyTile>(sh.vs[1], a.v.p, vbase, a.v.st, k0, r.seq.length, s.dim, a.codes, a.f, a.up);
+            __syncthreads();
+#pragma unroll 1
+            for (int kt = 0; kt < 2; ++kt) {
+                f32x16 x, dp, more;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = dp[i] = more[i] = 0.0f;
+#pragma unroll
+                for (int kk = 0; kk < 2 * DT; ++kk) {
+                    const u32x4 q = *reinterpret_cast<const u32x4 *>(a.qh + r.info * DP + 16 * kk + 8 * half);
+                    const u32x4 go = *reinterpret_cast<const u32x4 *>(a.gh + r.info * DP + 16 * kk + 8 * half);
+                    u32x4 f[1];
+                    read_rows(sh.ks[0], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
+                    x = mfma_f16(f[0], q, x);
+                    read_rows(sh.vs[0], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
+                    dp = mfma_f16(f[0], go, dp);
+                    read_rows(sh.vs[1], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
+                    more = mfma_f16(f[0], go, more);
+                }
+                attn_hide(sees, k0 + 32 * kt + 4 * half, x);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float p = exp2_fast(fmaf(x[i], scale2, -lse2)), rest = more[i] * (1.0f / kRestUp);
+                    x[i] = p * (of_k ? fmaf(dp[i] + rest, dp_by, -delta_by) : rest * dp_by);
+                }
+                if (!of_k) {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) most = larger(x[i], x[i + 1], most);
+                }
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    float ds[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) ds[j] = x[8 * kb + j];
+                    u32x4 pp[NP];
+                    f16_pieces<NP>(ds, pp);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        u32x4 f[1];
+                        read_columns(sh.ks[of_k], 32 * kt + 16 * kb, 32 * d, lane, f);
+#pragma unroll
+                        for (int w = NP - 1; w >= 0; --w) dq[d] = mfma_f16(f[0], pp[w], dq[d]);
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        if (of_k) times<DT>(dq, 1.0f / kRestUp);
+    }
+    // the factor is that of what there was without the rests
+    const float largest = __builtin_elementwise_maximum(most, __shfl_xor(most, 32));
+    bad |= !(largest <= kFactorMost) || (largest > 0.0f && largest < kFactorFloor<NP>);
+}
+
 // Returns whether the workgroup has to be computed with bf16 pieces.
 template <int NP, int DT>
 __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfShared<DT> &sh)
@@ -593,33 +684,30 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
                 dp = mfma_f16(f[0], go[kk], dp);
             }
             if (!all) attn_hide(sees, k0 + 32 * kt + 4 * half, x);
+            float top = most;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = exp2_fast(fmaf(x[i], scale2, -lse2)) * fmaf(dp[i], dp_by, -delta_by);
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) top = larger(x[i], x[i + 1], top);
+            if (__builtin_expect(__any(factor_off<NP>(top, top)), 0)) {
+                const float both = __builtin_elementwise_maximum(top, __shfl_xor(top, 32));
+                const int fall = factor_fall(both, both);
+                bad |= !(both < INFINITY);
+                factor -= fall;
+                dp_by = ldexpf(down, factor);
+                delta_by = ldexpf(delta, factor);
+                const float by = ldexpf(1.0f, -fall);
+                times<DT>(dq, by);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] *= by;
+                top = both * by;                                       // (the same in both lanes: what is small in one need not be in the other)
+            }
+            most = top;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                float ds[8], top;
-                for (int turn = 0;; ++turn) {
-                    top = most;
+                float ds[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float p = exp2_fast(fmaf(x[8 * kb + j], scale2, -lse2));
-                        ds[j] = p * fmaf(dp[8 * kb + j], dp_by, -delta_by);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; j += 2) top = larger(ds[j], ds[j + 1], top);
-                    if (__builtin_expect(!__any(factor_off<NP>(top, top)), 1)) break;
-                    if (turn == 1) {                                   // an infinity or NaN
-                        bad = true;
-                        break;
-                    }
-                    const float both = __builtin_elementwise_maximum(top, __shfl_xor(top, 32));
-                    const int fall = factor_fall(both, both);
-                    factor -= fall;
-                    dp_by = ldexpf(down, factor);
-                    delta_by = ldexpf(delta, factor);
-                    const float by = ldexpf(1.0f, -fall);
-                    times<DT>(dq, by);
-                    if (both < INFINITY) most = both * by;             // (the same in both lanes: what is small in one need not be in the other)
-                }
-                most = top;
+                for (int j = 0; j < 8; ++j) ds[j] = x[8 * kb + j];
                 u32x4 pp[NP];
                 f16_pieces<NP>(ds, pp);
 #pragma unroll
@@ -634,55 +722,12 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
     }
     if (r.live && lse2 < INFINITY && grow != kNoRow) {
         const float largest = __builtin_elementwise_maximum(most, __shfl_xor(most, 32));
-        bad |= ldexpf(dp_lost(high), factor + 20) > largest;
+        bad |= ldexpf(dp_lost_of_do(high), factor + 20) > largest;
     }
     if (__builtin_expect(half_flags(a, high, bad), 0)) return true;
-    if (__builtin_expect(high.k >> 31, 0)) {                                    // the same in the whole workgroup
-        times<DT>(dq, kRestUp);
-        const int64_t kbase = r.b * a.k.sb + r.kh * a.k.sh;
-#pragma unroll 1
-        for (int n = 0; n < count; ++n) {
-            const int tile = tiles.at(n), k0 = tile * kKeyTile;
-            if (!(highs.of(highs.k, k0, kKeyTile) >> 31)) continue;
-            kr.fetch(keys + static_cast<int64_t>(tile) * kKeyTile * DP);
-            vr.fetch(values + static_cast<int64_t>(tile) * kKeyTile * DP);
-            kr.put(sh.ks[0]);
-            vr.put(sh.vs[0]);
-            load_rests<DT, kKeyTile>(sh.ks[1], a.k.p, kbase, a.k.st, k0, r.seq.length, s.dim, a.codes, a.f, a.up);
-            __syncthreads();
-#pragma unroll 1
-            for (int kt = 0; kt < 2; ++kt) {
-                f32x16 x, dp;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
-#pragma unroll
-                for (int kk = 0; kk < 2 * DT; ++kk) {
-                    u32x4 f[1];
-                    read_rows(sh.ks[0], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
-                    x = mfma_f16(f[0], q[kk], x);
-                    read_rows(sh.vs[0], 32 * kt + (lane & 31), 16 * kk + 8 * half, f);
-                    dp = mfma_f16(f[0], go[kk], dp);
-                }
-                attn_hide(sees, k0 + 32 * kt + 4 * half, x);
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    float ds[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) ds[j] = exp2_fast(fmaf(x[8 * kb + j], scale2, -lse2)) * fmaf(dp[8 * kb + j], dp_by, -delta_by);
-                    u32x4 pp[NP];
-                    f16_pieces<NP>(ds, pp);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        u32x4 f[1];
-                        read_columns(sh.ks[1], 32 * kt + 16 * kb, 32 * d, lane, f);
-#pragma unroll
-                        for (int w = NP - 1; w >= 0; --w) dq[d] = mfma_f16(f[0], pp[w], dq[d]);
-                    }
-                }
-            }
-            __syncthreads();
-        }
-        times<DT>(dq, 1.0f / kRestUp);
+    if (__builtin_expect((high.k >> 31) | (high.v & 0xFFu), 0)) {             // the same in the whole workgroup
+        dq_rests<NP, DT>(a, opaque(id), high, sh, dq, factor, most, bad);
+        if (__syncthreads_or(bad)) return true;
     }
     const float last = bring_down<DT>(dq, grow == kNoRow ? 0 : -static_cast<int>(grow) - factor, s.scale * down);
     store_dq<DT>(a, r, dq, last);
@@ -724,6 +769,105 @@ __device__ __forceinline__ void load_row_rests(const AttnBwd &a, AttnTile<1, DT,
     }
 }
 
+// Rows that see a lane's key.
+struct SeenRows {
+    int first;
+    uint32_t count;
+};
+__device__ __forceinline__ SeenRows rows_that_see(const AttnShape &s, const KeyBlock &key)
+{
+    SeenRows seen{0, 0};
+    if (key.used) {
+        int64_t t0 = 0, t1 = s.q_len;
+        if (s.causal) t0 = max(t0, static_cast<int64_t>(key.key) - key.seq.first);
+        if (s.window && key.key >= s.sinks) {
+            t0 = max(t0, static_cast<int64_t>(key.key) - s.window + 1 - key.seq.first);
+            t1 = min(t1, static_cast<int64_t>(key.key) + s.window - key.seq.first);
+        }
+        if (t0 < t1) seen = SeenRows{static_cast<int>(t0 * s.group), static_cast<uint32_t>((t1 - t0) * s.group)};
+    }
+    return seen;
+}
+
+// What Q and dO lost, times 2^24, in dK and dV: over the tiles concerned.
+template <int NP, int DT>
+__device__ __forceinline__ void dkv_rests(const AttnBwd &a, uint32_t id, DkvHalfShared<DT> &sh, f32x16 (&dk)[DT], f32x16 (&dv)[DT], float least, float by)
+{
+    constexpr int kRows = kHalfRows<DT>, DP = 32 * DT;
+    const AttnShape &s = a.s;
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    const KeyBlock key = key_block<DT>(a, id);
+    const uint32_t bkh = key.b * s.kv_heads + key.kh;
+    const PackHighs highs(a, bkh);
+    const int64_t all_rows = info_rows(a), mine = (static_cast<int64_t>(bkh) * a.key_tiles * kKvKeys + key.key) * DP + 8 * half;
+    const uint16_t *queries = a.qh + key.info * DP, *gradients = a.gh + key.info * DP;
+    const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up), down17 = 0x1p-17f / a.up;
+    const SeenRows seen = rows_that_see(s, key);
+    times<DT>(dk, kRestUp);
+    times<DT>(dv, kRestUp);
+#pragma unroll 1
+    for (int row0 = key.first; row0 < key.last; row0 += kRows) {
+        if (!(highs.of(highs.q, row0, kRows) >> 31)) continue;
+        TileLoad<DT, kRows> load;
+        load.fetch(queries + static_cast<int64_t>(row0) * DP);
+        load.put(sh.qs[0]);
+        load.fetch(gradients + static_cast<int64_t>(row0) * DP);
+        load.put(sh.gs[0]);
+        load_row_rests<DT>(a, sh.qs[1], sh.gs[1], key, row0);
+        if (threadIdx.x < kRows) {
+            const int64_t at = key.info + row0 + threadIdx.x;
+            const float grow = a.info[kInfoGrow * all_rows + at];
+            sh.lse[0][threadIdx.x] = grow == kNoRow ? INFINITY : a.info[kInfoLse2 * all_rows + at] - (least - grow);
+            sh.delta[0][threadIdx.x] = a.info[kInfoScaledDelta * all_rows + at] * 0x1p-17f;
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int rt = 0; rt < kRows / 32; ++rt) {
+            f32x16 x, dp;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
+#pragma unroll
+            for (int kk = 0; kk < 2 * DT; ++kk) {
+                const u32x4 k = *reinterpret_cast<const u32x4 *>(a.kh + mine + 16 * kk), v = *reinterpret_cast<const u32x4 *>(a.vh + mine + 16 * kk);
+                u32x4 f[1];
+                read_rows(sh.qs[0], 32 * rt + (lane & 31), 16 * kk + 8 * half, f);
+                x = mfma_f16(f[0], k, x);
+                read_rows(sh.gs[0], 32 * rt + (lane & 31), 16 * kk + 8 * half, f);
+                dp = mfma_f16(f[0], v, dp);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int row = 32 * rt + 8 * (i / 4) + 4 * half + (i & 3);
+                const float score = static_cast<uint32_t>(row0 + row - seen.first) < seen.count ? x[i] : -INFINITY;
+                x[i] = exp2_fast(fmaf(score, scale2, -sh.lse[0][row])) * by;
+                dp[i] = x[i] * fmaf(dp[i], down17, -sh.delta[0][row]);
+            }
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                float p[8], ds[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[j] = x[8 * kb + j], ds[j] = dp[8 * kb + j];
+                u32x4 pp[NP], dd[NP];
+                f16_pieces<NP>(p, pp);
+                f16_pieces<NP>(ds, dd);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    u32x4 f[1];
+                    read_columns(sh.gs[1], 32 * rt + 16 * kb, 32 * d, lane, f);
+#pragma unroll
+                    for (int w = NP - 1; w >= 0; --w) dv[d] = mfma_f16(f[0], pp[w], dv[d]);
+                    read_columns(sh.qs[1], 32 * rt + 16 * kb, 32 * d, lane, f);
+#pragma unroll
+                    for (int w = NP - 1; w >= 0; --w) dk[d] = mfma_f16(f[0], dd[w], dk[d]);
+                }
+            }
+        }
+        __syncthreads();
+    }
+    times<DT>(dk, 1.0f / kRestUp);
+    times<DT>(dv, 1.0f / kRestUp);
+}
+
 template <int NP, int DT>
 __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfShared<DT> &sh)
 {
@@ -763,21 +907,7 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
     const float scale2 = s.scale == 0.0f ? 1.0f : fabsf(s.scale2) / (a.up * a.up), down = 1.0f / a.up;
     const float down17 = down * 0x1p-17f;
-    // rows that see the lane's key
-    int seen_from = 0;
-    uint32_t seen = 0;
-    if (key.used) {
-        int64_t t0 = 0, t1 = s.q_len;
-        if (s.causal) t0 = max(t0, static_cast<int64_t>(key.key) - key.seq.first);
-        if (s.window && key.key >= s.sinks) {
-            t0 = max(t0, static_cast<int64_t>(key.key) - s.window + 1 - key.seq.first);
-            t1 = min(t1, static_cast<int64_t>(key.key) + s.window - key.seq.first);
-        }
-        if (t0 < t1) {
-            seen_from = static_cast<int>(t0 * s.group);
-            seen = static_cast<uint32_t>((t1 - t0) * s.group);
-        }
-    }
+    const SeenRows seen = rows_that_see(s, key);
     float least = kNoRow, running = kNoRow, widest = -kNoRow;      // the smallest grow: of the sums, and (wave 0) of the rows read so far; the largest of those
     bool bad = false;
     int factor = kKeyFactor;
@@ -839,43 +969,46 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
             if (!all) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    x[i] = static_cast<uint32_t>(row0 + 32 * rt + 8 * (i / 4) + 4 * half + (i & 3) - seen_from) < seen ? x[i] : -INFINITY;
+                    x[i] = static_cast<uint32_t>(row0 + 32 * rt + 8 * (i / 4) + 4 * half + (i & 3) - seen.first) < seen.count ? x[i] : -INFINITY;
             }
+            float top = most, top_ds = most_ds;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int row = 32 * rt + 8 * g + 4 * half;
+                const f32x4 lse = *reinterpret_cast<const f32x4 *>(&sh.lse[buf][row]), delta = *reinterpret_cast<const f32x4 *>(&sh.delta[buf][row]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[4 * g + j] = exp2_fast(fmaf(x[4 * g + j], scale2, -lse[j])) * by;
+                    dp[4 * g + j] = x[4 * g + j] * fmaf(dp[4 * g + j], down17, -delta[j]);
+                }
+                top = larger(x[4 * g], x[4 * g + 1], larger(x[4 * g + 2], x[4 * g + 3], top));
+                top_ds = larger(dp[4 * g], dp[4 * g + 1], larger(dp[4 * g + 2], dp[4 * g + 3], top_ds));
+            }
+            if (__builtin_expect(__any(factor_off<NP>(__builtin_elementwise_maximum(top, top_ds), smaller(top, top_ds))), 0)) {
+                const float both = __builtin_elementwise_maximum(top, __shfl_xor(top, 32)), both_ds = __builtin_elementwise_maximum(top_ds, __shfl_xor(top_ds, 32));
+                const float higher = __builtin_elementwise_maximum(both, both_ds);
+                const int fall = factor_fall(higher, smaller(both, both_ds));
+                bad |= !(higher < INFINITY);
+                factor -= fall;
+                by = ldexpf(1.0f, factor);
+                const float lower = ldexpf(1.0f, -fall);
+                times<DT>(dk, lower);
+                times<DT>(dv, lower);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    x[i] *= lower;
+                    dp[i] *= lower;
+                }
+                top = both * lower;                                    // (the same in both lanes: what is small in one need not be in the other)
+                top_ds = both_ds * lower;
+            }
+            most = top;
+            most_ds = top_ds;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                float p[8], ds[8], top, top_ds;
-                for (int turn = 0;; ++turn) {
-                    top = most;
-                    top_ds = most_ds;
+                float p[8], ds[8];
 #pragma unroll
-                    for (int j0 = 0; j0 < 8; j0 += 4) {
-                        const int row = 32 * rt + 16 * kb + 2 * j0 + 4 * half;
-                        const f32x4 lse = *reinterpret_cast<const f32x4 *>(&sh.lse[buf][row]), delta = *reinterpret_cast<const f32x4 *>(&sh.delta[buf][row]);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            p[j0 + j] = exp2_fast(fmaf(x[8 * kb + j0 + j], scale2, -lse[j])) * by;
-                            ds[j0 + j] = p[j0 + j] * fmaf(dp[8 * kb + j0 + j], down17, -delta[j]);
-                        }
-                        top = larger(p[j0], p[j0 + 1], larger(p[j0 + 2], p[j0 + 3], top));
-                        top_ds = larger(ds[j0], ds[j0 + 1], larger(ds[j0 + 2], ds[j0 + 3], top_ds));
-                    }
-                    if (__builtin_expect(!__any(factor_off<NP>(__builtin_elementwise_maximum(top, top_ds), smaller(top, top_ds))), 1)) break;
-                    if (turn == 2) {                                   // an infinity or NaN
-                        bad = true;
-                        break;
-                    }
-                    const float both = __builtin_elementwise_maximum(top, __shfl_xor(top, 32)), both_ds = __builtin_elementwise_maximum(top_ds, __shfl_xor(top_ds, 32));
-                    const float higher = __builtin_elementwise_maximum(both, both_ds);
-                    const int fall = factor_fall(higher, smaller(both, both_ds));
-                    factor -= fall;
-                    by = ldexpf(1.0f, factor);
-                    const float lower = ldexpf(1.0f, -fall);
-                    times<DT>(dk, lower);
-                    times<DT>(dv, lower);
-                    if (higher < INFINITY) most = both * lower, most_ds = both_ds * lower;     // (the same in both lanes: what is small in one need not be in the other)
-                }
-                most = top;
-                most_ds = top_ds;
+                for (int j = 0; j < 8; ++j) p[j] = x[8 * kb + j], ds[j] = dp[8 * kb + j];
                 u32x4 pp[NP], dd[NP];
                 f16_pieces<NP>(p, pp);
                 f16_pieces<NP>(ds, dd);
@@ -897,68 +1030,9 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
     most_ds = __builtin_elementwise_maximum(most_ds, __shfl_xor(most_ds, 32));
     const float low = smaller(most, most_ds);
     bad |= widest - running > static_cast<float>(kGrowSpread) || (low > 0.0f && low < kFactorFloor<NP>);
-    bad |= most * dp_lost(high) * 0x1p3f > most_ds;                  // P dp_lost 2^-17 2^20
+    bad |= most * (dp_lost_of_do(high) + dp_lost_of_v(high)) * 0x1p3f > most_ds;      // P dp_lost 2^-17 2^20
     if (__builtin_expect(half_flags(a, high, bad), 0)) return true;
-    if (__builtin_expect(high.q >> 31, 0)) {                                    // the same in the whole workgroup
-        times<DT>(dk, kRestUp);
-        times<DT>(dv, kRestUp);
-#pragma unroll 1
-        for (int row0 = key.first; row0 < key.last; row0 += kRows) {
-            if (!(highs.of(highs.q, row0, kRows) >> 31)) continue;
-            fetch(row0);
-            qr.put(sh.qs[0]);
-            gr.put(sh.gs[0]);
-            load_row_rests<DT>(a, sh.qs[1], sh.gs[1], key, row0);
-            if (threadIdx.x < kRows) {
-                sh.lse[0][threadIdx.x] = info[2] == kNoRow ? INFINITY : info[0] - (least - info[2]);
-                sh.delta[0][threadIdx.x] = info[1] * 0x1p-17f;
-            }
-            __syncthreads();
-#pragma unroll 1
-            for (int rt = 0; rt < kRows / 32; ++rt) {
-                f32x16 x, dp;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
-#pragma unroll
-                for (int kk = 0; kk < 2 * DT; ++kk) {
-                    u32x4 f[1];
-                    read_rows(sh.qs[0], 32 * rt + (lane & 31), 16 * kk + 8 * half, f);
-                    x = mfma_f16(f[0], k[kk], x);
-                    read_rows(sh.gs[0], 32 * rt + (lane & 31), 16 * kk + 8 * half, f);
-                    dp = mfma_f16(f[0], v[kk], dp);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    x[i] = static_cast<uint32_t>(row0 + 32 * rt + 8 * (i / 4) + 4 * half + (i & 3) - seen_from) < seen ? x[i] : -INFINITY;
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    float p[8], ds[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int row = 32 * rt + 16 * kb + 8 * (j / 4) + 4 * half + (j & 3);
-                        p[j] = exp2_fast(fmaf(x[8 * kb + j], scale2, -sh.lse[0][row])) * by;
-                        ds[j] = p[j] * fmaf(dp[8 * kb + j], down17, -sh.delta[0][row]);
-                    }
-                    u32x4 pp[NP], dd[NP];
-                    f16_pieces<NP>(p, pp);
-                    f16_pieces<NP>(ds, dd);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        u32x4 f[1];
-                        read_columns(sh.gs[1], 32 * rt + 16 * kb, 32 * d, lane, f);
-#pragma unroll
-                        for (int w = NP - 1; w >= 0; --w) dv[d] = mfma_f16(f[0], pp[w], dv[d]);
-                        read_columns(sh.qs[1], 32 * rt + 16 * kb, 32 * d, lane, f);
-#pragma unroll
-                        for (int w = NP - 1; w >= 0; --w) dk[d] = mfma_f16(f[0], dd[w], dk[d]);
-                    }
-                }
-            }
-            __syncthreads();
-        }
-        times<DT>(dk, 1.0f / kRestUp);
-        times<DT>(dv, 1.0f / kRestUp);
-    }
+    if (__builtin_expect(high.q >> 31, 0)) dkv_rests<NP, DT>(a, opaque(id), sh, dk, dv, least, by);      // the same in the whole workgroup
     const int lose = least == kNoRow ? 0 : -static_cast<int>(least) - factor;
     const float klast = bring_down<DT>(dk, lose, fabsf(s.scale) * down * 131072.0f), vlast = bring_down<DT>(dv, lose, 1.0f);
     store_dkv<DT>(a, key, dk, dv, klast, vlast);
@@ -977,10 +1051,10 @@ __global__ __launch_bounds__(256, DT == 2 ? 2 : 1) void attn_bwd_half_kernel(Att
     } sh;
     if (blockIdx.x < a.key_blocks) {
         const uint32_t id = xcd_order(blockIdx.x, a.key_blocks);
-        if (__builtin_expect(dkv_half<NP, DT>(a, id, sh.kv), 0)) dkv_pieces<DT>(a, id, sh.kv_pieces);
+        if (__builtin_expect(dkv_half<NP, DT>(a, id, sh.kv), 0)) dkv_pieces<DT>(a, opaque(id), sh.kv_pieces);
     } else {
         const uint32_t id = xcd_order(blockIdx.x - a.key_blocks, a.row_blocks);
-        if (__builtin_expect(dq_half<NP, DT>(a, id, sh.q), 0)) dq_pieces<DT>(a, id, sh.q_pieces);
+        if (__builtin_expect(dq_half<NP, DT>(a, id, sh.q), 0)) dq_pieces<DT>(a, opaque(id), sh.q_pieces);
     }
 }
 

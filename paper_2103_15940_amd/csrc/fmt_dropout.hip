@@ -1,6 +1,8 @@
 // Dropout of a matrix (fmt_norm.h has the mathematics).  Bound by memory, and not far from the vector units' time for the generator:
 // 30011 x 4097 in binary16 codes, 492 MB, 93 us or 5.3 TB/s (a large elementwise pass: 6.2, with 16-byte accesses that odd rows do not
 // allow).  Loads and stores marked as used once gained nothing.
+#include <algorithm>
+
 #include "fmt_norm.h"
 
 namespace fmt {
@@ -11,9 +13,10 @@ constexpr int kDropThreads = 256, kDropRuns = 4;      // eights per thread
 
 template <int KIND, bool CODES, bool OUT>
 __global__ __launch_bounds__(kDropThreads) void dropout_kernel(const void *x, int64_t ldx, void *y, int64_t ldy, int64_t rows,
-                                                                int64_t cols, uint32_t blocks, Drop d, bool round, ElemFormat f)
+                                                                int64_t cols, uint32_t blocks, uint64_t before, Drop d, bool round, ElemFormat f)
 {
-    const uint64_t total = static_cast<uint64_t>(rows) * blocks, first = static_cast<uint64_t>(blockIdx.x) * (kDropThreads * kDropRuns);
+    // (before: eights of the launches before this one)
+    const uint64_t total = static_cast<uint64_t>(rows) * blocks, first = before + static_cast<uint64_t>(blockIdx.x) * (kDropThreads * kDropRuns);
     const uint64_t row0 = first / blocks;
     const uint32_t at0 = static_cast<uint32_t>(first - row0 * blocks);
     RawEight<CODES> raw[kDropRuns];
@@ -64,12 +67,15 @@ int launch_dropout(const void *x, int64_t ldx, void *y, int64_t ldy, int64_t row
     Drop drop = make_drop(d);
     drop.rng = d.rng;
     const uint32_t blocks = static_cast<uint32_t>((cols + 7) / 8);
-    const uint64_t grid = (static_cast<uint64_t>(rows) * blocks + kDropThreads * kDropRuns - 1) / (kDropThreads * kDropRuns);
-    if (grid > 0x7FFFFFFFull) return FMT_ERR_SHAPE;
+    const uint64_t total = static_cast<uint64_t>(rows) * blocks, each = kDropThreads * kDropRuns, most = most_workgroups(kDropThreads);
     with_kind(f, store, result, [&](auto kind, auto in, auto out) {
-        dropout_kernel<decltype(kind)::value, decltype(in)::value, decltype(out)::value>
-            <<<dim3(static_cast<uint32_t>(grid)), dim3(kDropThreads), 0, stream>>>(x, ldx, y, ldy, rows, cols, blocks, drop,
-                                                                                   result != FMT_RESULT_F32, f);
+        for (uint64_t before = 0; before < total;) {
+            const uint64_t grid = std::min((total - before + each - 1) / each, most);
+            dropout_kernel<decltype(kind)::value, decltype(in)::value, decltype(out)::value>
+                <<<dim3(static_cast<uint32_t>(grid)), dim3(kDropThreads), 0, stream>>>(x, ldx, y, ldy, rows, cols, blocks, before, drop,
+                                                                                       result != FMT_RESULT_F32, f);
+            before += grid * each;
+        }
     });
     FMT_HIP_CHECK(hipGetLastError());
     return FMT_OK;

@@ -180,6 +180,9 @@ inline ElemFormat make_elem_format(fmt_format_t f, const QuantParams &p)
     return ElemFormat{p, f.denorm == 0, codec};
 }
 
+// Workgroups of so many threads that one launch may have: its threads are counted in 32 bits, and more of them wrap without an error.
+constexpr int64_t most_workgroups(int threads) { return (((int64_t)1 << 32) - 1) / threads; }
+
 // Row-wise operators (fmt_dropout.hip, fmt_norm_fwd.hip, fmt_norm_bwd.hip).
 struct LayerNorm {
     int64_t rows, cols;

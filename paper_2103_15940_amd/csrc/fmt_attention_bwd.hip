@@ -196,6 +196,8 @@ __global__ __launch_bounds__(256) void attn_parts_kernel(AttnBwd a)
 
 }  // namespace
 
+constexpr int64_t kMostWords = (int64_t)1 << 31;      // of scratch for operands, beyond which a call of several sequences goes in two
+
 int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &k, const AttnView &v, const AttnView &o, const AttnView &go,
                          const float *lse, const AttnView &dq, const AttnView &dk, const AttnView &dv, int32_t store, int32_t result,
                          const ElemFormat &f, fmt_format_t fmt, hipStream_t stream)
@@ -232,11 +234,28 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
     a.parts = static_cast<int32_t>(parts);
     a.part_keys = static_cast<int32_t>(std::min<int64_t>(s.k_len, static_cast<int64_t>(a.part_tiles) * kKvKeys));
     const int64_t key_blocks = (a.part_tiles * parts + a.key_tiles - a.part_tiles) * bkh, row_blocks = static_cast<int64_t>(a.row_tiles) * s.kv_heads * s.batch;
-    if (key_blocks + row_blocks > 0x1FFFFFFF) return FMT_ERR_SHAPE;
+    const bool half = attention_half(fmt, s);
+    const int64_t width = s.dim <= 64 ? 64 : 128;
+    const int64_t prows = bkh * a.row_tiles * kRowTile, pkeys = bkh * a.key_tiles * kKvKeys, whole = static_cast<int64_t>(s.batch) * a.part_keys * s.kv_heads * s.dim;
+    const int64_t operands = half ? (prows + pkeys) * width : 0;       // words: two tensors of half a word
+    const bool too_many = std::max(key_blocks + row_blocks, 4 * bkh * (a.row_tiles + a.key_tiles)) > most_workgroups(256) ||
+                          (parts > 1 && 2 * whole > most_workgroups(1));
+    if (too_many || operands + 4 * prows > kMostWords) {
+        // in two calls, if there are two sequences
+        if (s.batch > 1) {
+            const int32_t first = s.batch / 2;
+            const int64_t in = store == FMT_STORE_CODE16 ? 2 : 4, out = result == FMT_RESULT_CODE16 ? 2 : 4;
+            rc = launch_attention_bwd(attn_from(s, 0, first), q, k, v, o, go, lse, dq, dk, dv, store, result, f, fmt, stream);
+            if (rc != FMT_OK) return rc;
+            return launch_attention_bwd(attn_from(s, first, s.batch - first), attn_from(q, first, in), attn_from(k, first, in), attn_from(v, first, in),
+                                        attn_from(o, first, out), attn_from(go, first, out), lse + static_cast<int64_t>(first) * s.heads * s.q_len,
+                                        attn_from(dq, first, out), attn_from(dk, first, out), attn_from(dv, first, out), store, result, f, fmt, stream);
+        }
+        if (too_many) return FMT_ERR_SHAPE;
+    }
     a.key_blocks = static_cast<uint32_t>(key_blocks);
     a.row_blocks = static_cast<uint32_t>(row_blocks);
     if (key_blocks + row_blocks == 0) return FMT_OK;
-    const bool half = attention_half(fmt, s);
     a.codes = store == FMT_STORE_CODE16;
     a.gcodes = result == FMT_RESULT_CODE16;
     a.check = fmt.e > 5;
@@ -245,10 +264,8 @@ int launch_attention_bwd(const AttnShape &s, const AttnView &q, const AttnView &
     a.limit = a.check && half ? ldexpf(1.0f, score_limit(s)) : 0.0f;
 
     // scratch: fp16 operands first (rows of 64 or 128 bytes), then words
-    const int64_t width = s.dim <= 64 ? 64 : 128;
-    const int64_t prows = bkh * a.row_tiles * kRowTile, pkeys = bkh * a.key_tiles * kKvKeys, whole = static_cast<int64_t>(s.batch) * a.part_keys * s.kv_heads * s.dim;
     static_assert(kRowTile / kPackRows == 4 && kKvKeys / kPackRows == 4);
-    const int64_t operands = half ? (prows + pkeys) * width : 0, nhighs = half ? 4 * bkh * (a.row_tiles + 2 * a.key_tiles) : 0;      // words: two tensors of half a word
+    const int64_t nhighs = half ? 4 * bkh * (a.row_tiles + 2 * a.key_tiles) : 0;
     const int64_t nparts = a.parts > 1 ? 2 * a.parts * whole : 0;
     float *scratch = nullptr;
     rc = get_acc_scratch(stream, static_cast<size_t>(operands + 4 * prows + nhighs + nparts + 1) * sizeof(float), &scratch);

@@ -132,7 +132,16 @@ int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &
     AttnFwd a{s, q, k, v, o, lse, result, static_cast<int32_t>(splits), nullptr, check ? kHalfUp : 1.0f, static_cast<int32_t>(row_tiles),
               store == FMT_STORE_CODE16, make_half_codes(fmt, s, store), f};
     const int64_t all_rows = static_cast<int64_t>(s.batch) * s.heads * s.q_len, grid = work * splits;
-    if (grid > 0x7FFFFFFF) return FMT_ERR_SHAPE;
+    if (grid > most_workgroups(256)) {                     // in two calls
+        if (s.batch == 1) return FMT_ERR_SHAPE;
+        const int32_t first = s.batch / 2;
+        const int64_t in = store == FMT_STORE_CODE16 ? 2 : 4, out = result == FMT_RESULT_CODE16 ? 2 : 4;
+        rc = launch_attention_fwd(attn_from(s, 0, first), q, k, v, o, lse, store, result, f, fmt, stream);
+        if (rc != FMT_OK) return rc;
+        return launch_attention_fwd(attn_from(s, first, s.batch - first), attn_from(q, first, in), attn_from(k, first, in), attn_from(v, first, in),
+                                    attn_from(o, first, out), lse ? lse + static_cast<int64_t>(first) * s.heads * s.q_len : nullptr, store, result, f,
+                                    fmt, stream);
+    }
     if (splits > 1) {
         rc = get_acc_scratch(stream, static_cast<size_t>(splits * all_rows * (s.dim + 2)) * sizeof(float), &a.part);
         if (rc != FMT_OK) return rc;

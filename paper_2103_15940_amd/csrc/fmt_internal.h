@@ -212,6 +212,19 @@ struct AttnShape {
     const int32_t *k_lens, *q_pos;
 };
 
+// The same tensor from sequence b on; its elements have `size` bytes.
+inline AttnView attn_from(const AttnView &v, int64_t b, int64_t size) { return AttnView{static_cast<const char *>(v.p) + b * v.sb * size, v.sb, v.st, v.sh}; }
+
+// `count` sequences from b on.
+inline AttnShape attn_from(const AttnShape &s, int32_t b, int32_t count)
+{
+    AttnShape t = s;
+    t.batch = count;
+    if (t.k_lens) t.k_lens += b;
+    if (t.q_pos) t.q_pos += b;
+    return t;
+}
+
 constexpr int kAttnMaxDim = 128;
 int launch_attention_fwd(const AttnShape &s, const AttnView &q, const AttnView &k, const AttnView &v, const AttnView &o, float *lse,
                          int32_t store, int32_t result, const ElemFormat &f, fmt_format_t fmt, hipStream_t stream);

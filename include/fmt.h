@@ -618,7 +618,7 @@ typedef struct fmt_attention {
     int32_t batch, heads, kv_heads, q_len, k_len, dim;
     int32_t causal;        /* 0 or 1 */
     int32_t window, sinks; /* 0 <= window, sinks < 2^30; window == 0: no window */
-    float scale;           /* finite */
+    float scale;           /* |scale| < 2^90 */
     const int32_t *k_lens; /* device, batch values, or NULL */
     const int32_t *q_pos;  /* device, batch values in (-2^30, 2^30), or NULL */
 } fmt_attention_t;

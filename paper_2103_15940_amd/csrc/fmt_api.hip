@@ -888,7 +888,7 @@ static int check_attention(const fmt_attention_t &a, std::initializer_list<AttnT
     if (a.batch > 65535 || a.kv_heads > 65535 || a.heads % a.kv_heads != 0 || a.q_len >= lim || a.k_len >= lim) return FMT_ERR_SHAPE;
     if ((int64_t)a.q_len * std::max(a.heads / a.kv_heads, 1) >= lim || (int64_t)a.batch * a.heads > ((int64_t)1 << 40) / std::max(a.q_len, 1))
         return FMT_ERR_SHAPE;
-    if ((a.causal != 0 && a.causal != 1) || a.window < 0 || a.window >= lim || a.sinks < 0 || a.sinks >= lim || !std::isfinite(a.scale))
+    if ((a.causal != 0 && a.causal != 1) || a.window < 0 || a.window >= lim || a.sinks < 0 || a.sinks >= lim || !(std::fabs(a.scale) < 0x1p90f))
         return FMT_ERR_RANGE;
     for (const AttnTensor &t : tensors)
         if ((rc = check_attn_tensor(t, a)) != FMT_OK) return rc;

@@ -863,17 +863,40 @@ static int check_attn_tensor(const AttnTensor &t, const fmt_attention_t &a)
     return aligned(t.v.data, t.size) ? FMT_OK : FMT_ERR_ALIGN;
 }
 
-// Whether two tensors share an element: their spans meet, and they are not slices side by side of the tokens of one tensor.
+// Whether two tensors may share an element.  They do not where their spans do not meet, nor as slices side by side, at some dimension, of one tensor:
+// with the same strides there, and both within one step of each longer stride.
 static bool attn_clash(const AttnTensor &s, const AttnTensor &t, const fmt_attention_t &a)
 {
     if (s.empty(a) || t.empty(a)) return false;
     if (!overlap(s.v.data, s.size * (size_t)s.extent(a), t.v.data, t.size * (size_t)t.extent(a))) return false;
-    const bool alike = s.size == t.size && s.v.stride_t == t.v.stride_t && (a.batch == 1 || s.v.stride_b == t.v.stride_b);
-    const int64_t size = (int64_t)s.size, row = size * s.v.stride_t;
-    const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(t.v.data) - reinterpret_cast<uintptr_t>(s.v.data));
-    const int64_t swide = size * ((s.heads - 1) * s.v.stride_h + a.dim), twide = size * ((t.heads - 1) * t.v.stride_h + a.dim);
-    const bool batches_apart = a.batch == 1 || s.v.stride_b >= std::max(s.tokens, t.tokens) * s.v.stride_t;
-    return !(alike && batches_apart && (apart >= 0 ? apart >= swide && apart + twide <= row : -apart >= twide && -apart + swide <= row));
+    if (s.size != t.size) return true;
+    if (reinterpret_cast<uintptr_t>(t.v.data) < reinterpret_cast<uintptr_t>(s.v.data)) return attn_clash(t, s, a);
+    const int64_t bytes = (int64_t)(reinterpret_cast<uintptr_t>(t.v.data) - reinterpret_cast<uintptr_t>(s.v.data)), size = (int64_t)s.size;
+    if (bytes % size != 0) return true;
+    const int64_t apart = bytes / size;
+    struct Dim {
+        int64_t stride, ns, nt;
+    } dims[3];
+    int count = 0;
+    const int64_t ss[3] = {s.v.stride_b, s.v.stride_t, s.v.stride_h}, ts[3] = {t.v.stride_b, t.v.stride_t, t.v.stride_h};
+    const int64_t ns[3] = {a.batch, s.tokens, s.heads}, nt[3] = {a.batch, t.tokens, t.heads};
+    for (int i = 0; i < 3; ++i) {
+        if (ns[i] == 1 && nt[i] == 1) continue;
+        if (ns[i] > 1 && nt[i] > 1 && ss[i] != ts[i]) return true;
+        dims[count++] = Dim{ns[i] > 1 ? ss[i] : ts[i], ns[i], nt[i]};
+    }
+    std::sort(dims, dims + count, [](const Dim &x, const Dim &y) { return x.stride < y.stride; });
+    int64_t se[4] = {a.dim}, te[4] = {a.dim};          // extents of the dimensions below
+    for (int i = 0; i < count; ++i) {
+        se[i + 1] = se[i] + (dims[i].ns - 1) * dims[i].stride;
+        te[i + 1] = te[i] + (dims[i].nt - 1) * dims[i].stride;
+    }
+    for (int i = count - 1; i >= 0; --i) {
+        const int64_t step = dims[i].stride, in = step > 0 ? apart % step : 0;
+        if (in >= se[i] && in + te[i] <= step) return false;
+        if (se[i] > step || apart + te[i] > step) return true;
+    }
+    return apart < a.dim;
 }
 
 // What both directions check; *e and *s are filled.

@@ -112,38 +112,6 @@ __device__ __forceinline__ void load8(const void *x, int64_t at, int count, floa
     }
 }
 
-// The first `count` of eight results to y[at].  RESULT: FMT_RESULT_*; ROUNDED: the values are the format's already.
-template <int RESULT, bool ROUNDED = false>
-__device__ __forceinline__ void store8(void *y, int64_t at, int count, float (&v)[8], const ElemFormat &f)
-{
-    if (RESULT != FMT_RESULT_F32 && !ROUNDED) round_values(v, f);
-    if constexpr (RESULT == FMT_RESULT_CODE16) {
-        uint16_t c[8];
-        encode_values(v, c, f);
-        uint16_t *d = static_cast<uint16_t *>(y) + at;
-        if (count >= 8) {
-            u16x8_any w;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = c[i];
-            *reinterpret_cast<u16x8_any *>(d) = w;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < count) d[i] = c[i];
-        }
-    } else {
-        float *d = static_cast<float *>(y) + at;
-        if (count >= 8) {
-            *reinterpret_cast<f32x4_any *>(d) = f32x4_any{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4_any *>(d + 4) = f32x4_any{v[4], v[5], v[6], v[7]};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < count) d[i] = v[i];
-        }
-    }
-}
-
 // The same with the type known at run time (uniform).
 __device__ __forceinline__ void load8_any(const void *x, int64_t at, int count, float (&v)[8], bool codes, const ElemFormat &f)
 {

@@ -444,9 +444,9 @@ __device__ __forceinline__ u32x4 half_signed(u32x4 q, float scale)
 }
 
 // Forward the running maximum stays where it is until a score passes it by 2^4 (a wave of 32 rows would otherwise multiply its sums with some row's factor at
-// almost every tile), so P can reach 2^4, and is taken times 2^11: weights keep 22 bits down to 2^-14 of a row's largest, and 11 down to 2^-25.  (With
-// 2^8 and 2^6 a row whose largest weight meets a V of zero had five bits less.)
-constexpr float kFwdUp = 11.0f, kFwdSlack = 4.0f;
+// almost every tile), so P can reach 2^4, and is taken times 2^8: weights keep 22 bits down to 2^-11 of a row's largest, and 11 down to 2^-22.  (The factor comes
+// out of the exponential, whose argument has fewer bits the larger it is: with 2^11 ordinary rows' errors were half as large again.)
+constexpr float kFwdUp = 8.0f, kFwdSlack = 4.0f;
 
 // Whether a workgroup has to be computed with bf16 pieces: in all of its threads.  Every thread calls it.  high, high_value: what raw_half left.
 template <bool CODES>

@@ -421,7 +421,8 @@ __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (hal
     }
     sum += __shfl_xor(sum, 32);
     const float over = sum == 0.0f ? 0.0f : 1.0f / (sum * a.up);
-    if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, top - kFwdUp, sum);
+    // (the sum without P's factor: its logarithm would have fewer bits)
+    if (live) fwd_store<DT>(a, o, split, b, t, head, half, over, top, sum * exp2_fast(-kFwdUp));
 }
 
 }  // namespace

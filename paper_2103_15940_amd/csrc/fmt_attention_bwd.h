@@ -512,7 +512,7 @@ __device__ __forceinline__ void load_rests(AttnTile<1, DT, ROWS> &t, const void 
 {
     constexpr int kEights = 4 * DT;
     bool ignore = false;
-#pragma unroll 1
+#pragma unroll 2
     for (int i = 0; i < ROWS * kEights / 256; ++i) {
         const int n = threadIdx.x + 256 * i, row = n / kEights, col = (n % kEights) * 8;
         float v[8];
@@ -560,11 +560,11 @@ __device__ __forceinline__ void dq_rests(const AttnBwd &a, uint32_t id, const Hi
         for (int n = 0; n < tiles.count(); ++n) {
             const int tile = tiles.at(n), k0 = tile * kKeyTile;
             if (!(of_k ? highs.of(highs.k, k0, kKeyTile) >> 31 : highs.of(highs.v, k0, kKeyTile) & 0xFFu)) continue;
-            TileLoad<DT, kKeyTile> load;
-            load.fetch(keys + static_cast<int64_t>(tile) * kKeyTile * DP);
-            load.put(sh.ks[0]);
-            load.fetch(values + static_cast<int64_t>(tile) * kKeyTile * DP);
-            load.put(sh.vs[0]);
+            TileLoad<DT, kKeyTile> k_load, v_load;
+            k_load.fetch(keys + static_cast<int64_t>(tile) * kKeyTile * DP);
+            v_load.fetch(values + static_cast<int64_t>(tile) * kKeyTile * DP);
+            k_load.put(sh.ks[0]);
+            v_load.put(sh.vs[0]);
             load_rests<DT, kKeyTile>(sh.ks[1], a.k.p, kbase, a.k.st, k0, r.seq.length, s.dim, a.codes, a.f, a.up);
             load_rests<DT, kKeyTile>(sh.vs[1], a.v.p, vbase, a.v.st, k0, r.seq.length, s.dim, a.codes, a.f, a.up);
             __syncthreads();
@@ -722,7 +722,8 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
     }
     if (r.live && lse2 < INFINITY && grow != kNoRow) {
         const float largest = __builtin_elementwise_maximum(most, __shfl_xor(most, 32));
-        bad |= ldexpf(dp_lost_of_do(high), factor + 20) > largest;
+        // (beside a delta 2^24 times as large dP loses no more than it does in fp32; dS of a row that sees one key is nothing but rounding)
+        bad |= ldexpf(dp_lost_of_do(high), factor + 20) > largest && dp_lost_of_do(high) > fabsf(delta) * 0x1p-24f;
     }
     if (__builtin_expect(half_flags(a, high, bad), 0)) return true;
     if (__builtin_expect((high.k >> 31) | (high.v & 0xFFu), 0)) {             // the same in the whole workgroup
@@ -749,7 +750,7 @@ __device__ __forceinline__ void load_row_rests(const AttnBwd &a, AttnTile<1, DT,
     constexpr int kEights = 4 * DT;
     const AttnShape &s = a.s;
     bool ignore = false;
-#pragma unroll 1
+#pragma unroll
     for (int i = 0; i < kHalfRows<DT> * kEights / 256; ++i) {
         const int n = threadIdx.x + 256 * i, r = n / kEights, col = (n % kEights) * 8, row = row0 + r;
         float q[8], g[8];
@@ -762,7 +763,7 @@ __device__ __forceinline__ void load_row_rests(const AttnBwd &a, AttnTile<1, DT,
             load8_any(a.go.p, key.b * a.go.sb + at.t * a.go.st + head * a.go.sh + col, count, g, a.gcodes, a.f);
             const float grow = a.info[kInfoGrow * info_rows(a) + key.info + row];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] = grow == kNoRow ? 0.0f : ldexpf(g[j], static_cast<int>(grow));
+            for (int j = 0; j < 8; ++j) g[j] = ldexpf(g[j], grow == kNoRow ? 0 : static_cast<int>(grow));
         }
         *reinterpret_cast<u32x4 *>(&qs.e[0][r][col]) = half_signed(half_rest(q, a.up, ignore), s.scale);
         *reinterpret_cast<u32x4 *>(&gs.e[0][r][col]) = half_rest(g, 1.0f, ignore);
@@ -808,11 +809,11 @@ __device__ __forceinline__ void dkv_rests(const AttnBwd &a, uint32_t id, DkvHalf
 #pragma unroll 1
     for (int row0 = key.first; row0 < key.last; row0 += kRows) {
         if (!(highs.of(highs.q, row0, kRows) >> 31)) continue;
-        TileLoad<DT, kRows> load;
-        load.fetch(queries + static_cast<int64_t>(row0) * DP);
-        load.put(sh.qs[0]);
-        load.fetch(gradients + static_cast<int64_t>(row0) * DP);
-        load.put(sh.gs[0]);
+        TileLoad<DT, kRows> q_load, g_load;
+        q_load.fetch(queries + static_cast<int64_t>(row0) * DP);
+        g_load.fetch(gradients + static_cast<int64_t>(row0) * DP);
+        q_load.put(sh.qs[0]);
+        g_load.put(sh.gs[0]);
         load_row_rests<DT>(a, sh.qs[1], sh.gs[1], key, row0);
         if (threadIdx.x < kRows) {
             const int64_t at = key.info + row0 + threadIdx.x;

@@ -4,9 +4,10 @@
 // P is made again from Q, K and lse.  Two kernels: one takes rows and adds up dQ over keys, the other takes keys and adds up dK and dV over
 // rows, so that every sum is in one workgroup's accumulators, in a fixed order, at the price of S and dP twice (7 products instead of 5).
 //
-// Measured: 4 x 1024 tokens, 16 heads of 64, window 256 and 4 sinks, bfloat16: 60 us for 23 GFLOP (of the five products), beside 15 for
-// the packing and 6 for the sinks' parts.  Bound by the vector units and by waiting: registers leave two waves to a SIMD, and between two products
-// lie an exponential, the factors of dS and the conversions of every score.
+// Measured: 4 x 1024 tokens, 16 heads of 64, window 256 and 4 sinks, bfloat16: 65 us for the 9.5 GFLOP of five products over the pairs that are
+// seen (146 TFLOP/s), beside 16 for the packing and 6 for the sinks' parts.  Bound by the vector units and by waiting (the matrix cores are busy for 19 % of
+// the time, LDS for 20 %; waves wait for 43 % of theirs): registers leave two waves to a SIMD, and between two products
+// lie an exponential, the factors of P and dS and the conversions of every score.
 #pragma once
 
 #include "fmt_attention.h"
@@ -505,6 +506,9 @@ struct TileLoad {
     }
 };
 
+// Second runs cost as much as a first: one channel of K or V of 2^-30, so that every tile has some: 4096 tokens, 8 heads of 128, 1/6/9: 436 -> 1147 us,
+// and 2319 with pieces of bf16 throughout (V of 200).  A few lost elements cost a few microseconds at the end of the workgroups that read them.
+//
 // What was cut of tokens [first, first + ROWS) of one head (load_tokens).
 template <int DT, int ROWS>
 __device__ __forceinline__ void load_rests(AttnTile<1, DT, ROWS> &t, const void *x, int64_t base, int64_t stride, int first, int end, int dim, bool codes,

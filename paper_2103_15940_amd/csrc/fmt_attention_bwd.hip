@@ -56,7 +56,7 @@ __device__ __forceinline__ int lanes_total(int n)
 
 // What the products need: of 32 rows delta = sum over the head's columns of R(dO) O, lse, and with HALF R(Q) and R(dO) as fp16 operands; with HALF
 // also of 32 keys R(K) and R(V).  4 DT lanes per row, 8 columns each.  One pass over the tensors, whose tiles are then read many times.
-// (42 MB read and 34 written for 4 x 1024 tokens with 16 heads of 64, 15 us: 4096 workgroups of one pass each.)
+// (42 MB read and 34 written for 4 x 1024 tokens with 16 heads of 64, 16 us: 4096 workgroups of one pass each.)
 template <int DT, bool HALF>
 __global__ __launch_bounds__(256) void attn_pack_kernel(AttnBwd a)
 {

@@ -28,8 +28,9 @@ struct FwdBlock {
 };
 
 // Workgroups of a causal mask differ in their keys, and with two to a compute unit, of which an XCD has 32, its workgroups n and n + 32 meet
-// in one: the second 32 go in reverse, so that long ones meet short ones (2 x 4096 tokens, 8 heads of 128: 188 -> 158 us).  Where there are
-// more, the later ones go where there is room, and the turn gained nothing (16 heads of 64: 162 -> 169).
+// in one: the second 32 go in reverse, so that long ones meet short ones (binary16, 8 heads of 128: 2 x 4096 tokens 170 -> 139 us, 8 x 1024
+// 50 -> 41, 1 x 8192 265 -> 250; of 64: 2 x 4096 111 -> 85).  Where there are more, the later ones go where there is room, and a turn gained
+// nothing (16 heads of 64: 162 -> 169).
 __device__ __forceinline__ uint32_t fwd_order(const AttnFwd &a, uint32_t i, uint32_t n)
 {
     constexpr uint32_t kUnits = 32;
@@ -201,9 +202,11 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnFwd a)
 // The same on operands of one fp16 value each, P in NP pieces of fp16.  The next tile's elements are on their way from memory while a
 // tile is computed; they are rounded and converted on their way into the other of two LDS buffers, so a tile costs one barrier.
 //
-// Measured: 16384 tokens, 8 heads over 2, head size 128, window 2048 and 16 sinks in binary16: 215 to 229 us, 570 to 600 TFLOP/s of S and O
-// (with both pieces of P 850 to 900; a large product reaches 1282).  Bound by LDS reads (the transposed ones take 7.3 cycles for 512 bytes,
-// the others 8 for 1024) and by the exponentials, conversions and sums between the two products, at two workgroups per compute unit.
+// Measured: 16384 tokens, 8 heads over 2, head size 128, window 2048 and 16 sinks in binary16: 211 to 231 us, 560 to 610 TFLOP/s of S and O
+// (with both pieces of P 840 to 920; a large product reaches 1282).  The matrix cores are busy for 50 % of the time, LDS for 42 % (two fifths of that bank
+// conflicts), and between the two products lie exponentials, conversions and sums, at two workgroups per compute unit.
+// What V lost to fp16 is added after the tiles: with one channel of 2^-30, so that every tile has some, the call takes 2.3 times as long, and computed again
+// with pieces of bf16 3.2 times (4096 tokens, 8 heads of 128, 1/6/9: 267, 617, 858 us).
 // Short sequences (32 x 128 tokens, 12 heads of 64) are a chain of two tiles: 18 us against 7 for their bytes.
 template <int NP, int DT, int KIND>
 __global__ __launch_bounds__(256, DT == 2 ? (half_is_codes(KIND) ? 3 : 2) : (half_is_codes(KIND) ? 2 : 1)) void attn_fwd_half_kernel(AttnFwd a)

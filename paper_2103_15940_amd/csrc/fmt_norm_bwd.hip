@@ -5,7 +5,7 @@
 // adds the records in a fixed order.  (Atomic additions would save that kernel, and give other bits every time.)
 //
 // Measured: 50001 x 768 in fp32, 461 MB: 91 us, 5.1 TB/s, and 4 to 5 us for the records; bound by memory.  4096 x 1024 in bfloat16: 15 us and 4,
-// eight rows per wave one after the other.
+// two rows per wave, one after the other, with eight waves on a compute unit.
 #include "fmt_norm.h"
 
 namespace fmt {

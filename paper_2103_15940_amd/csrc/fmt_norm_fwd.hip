@@ -4,7 +4,8 @@
 // before the first is used: a wave has one row, so its time is one trip to memory, two reductions and the stores.
 //
 // Measured: 4096 x 1024 in bfloat16 with residual and dropout 14 us (33.6 MB: 5.4 at the rate of a large elementwise pass): all 1024 workgroups
-// are on the card at once, so reads, generator and writes come one after the other for all of them.  32 x 1024: 5 us, the chain alone.
+// are on the card at once, so reads, generator and writes come one after the other for all of them.  128 x 128 in 1/6/9, fp32: 5.2 us, 32 x 1024:
+// 6.5, the chain alone.
 #include <algorithm>
 
 #include "fmt_norm.h"

@@ -611,7 +611,7 @@ int fmt_layernorm_bwd(int64_t rows, int64_t cols, const void *dy, int64_t lddy, 
  * below 2^-33 may be cut, where the scale lets them count for no more).  P = exp(S - lse) and dS are held to 22 bits, and to 11
  * where m <= 7 and the result is rounded to the format anyway.  What is finer than 2^-32 of the largest P of its row in O, or
  * than 2^-20 (2^-15 with 11 bits) of the largest dS of its row in dQ or of the largest P and dS of its key in dK and dV, may be lost;
- * P below 2^-126 is 0.
+ * P below 2^-126 is 0, and so may dS be below 2^-70 of the largest |dO| of its row.
  * Sums are taken in an order that depends on the sizes and the GPU alone.
  */
 typedef struct fmt_attention {

@@ -418,25 +418,30 @@ template <int NP>
 constexpr float kFactorFloor = NP == 2 ? 0x1p-5f : 0x1p-10f;
 
 // Whether a factor has to change: the larger of its largest products has passed, or is NaN, or the smaller one is small and there is room.
-// (dK's dS share the factor of dV's P.)
+// (dK's dS share the factor of dV's P.)  What is below `least` is taken for nothing: with a factor that brought it up, other products would overflow
+// (a row's dP comes to 2^38 at most, in the units that dS is held in, and is multiplied by the factor before P).
+constexpr float kRowLeast = 0x1p-60f, kKeyLeast = 0x1p-80f;
 template <int NP>
-__device__ __forceinline__ bool factor_off(float high, float low) { return !(high <= kFactorMost) || (low < kFactorFloor<NP> && low > 0.0f && high < 1024.0f); }
+__device__ __forceinline__ bool factor_off(float high, float low, float least)
+{
+    return !(high <= kFactorMost) || (low < kFactorFloor<NP> && low > least && high < 1024.0f);
+}
 
 // By how many binades the factors of a wave fall (rise: negative).  When one changes, others that are low rise as well, and those that have seen
 // nothing go with one that rises, so that few changes follow.
-__device__ __forceinline__ int factor_fall(float high, float low)
+__device__ __forceinline__ int factor_fall(float high, float low, float least)
 {
-    int fall = high > kFactorMost ? exponent_of(high) - 11 : low > 0.0f && low < 64.0f ? min(max(exponent_of(low) - 9, exponent_of(high) - 11), 0) : 0;
+    int fall = high > kFactorMost ? exponent_of(high) - 11 : low > least && low < 64.0f ? min(max(exponent_of(low) - 9, exponent_of(high) - 11), 0) : 0;
     if (!(high < INFINITY)) fall = 0;
     const uint64_t rising = __ballot(fall < 0);
     if (rising) {
         const int one = __builtin_amdgcn_readlane(fall, __builtin_ctzll(rising));
-        if (high == 0.0f) fall = one;
+        if (high <= least) fall = max(one, -20);
     }
     return fall;
 }
-// The smaller of two largest products that are not zero.
-__device__ __forceinline__ float smaller(float a, float b) { return b > 0.0f ? fminf(a, b) : a; }
+// The smaller of two largest products, where the second is not nothing.
+__device__ __forceinline__ float smaller(float a, float b) { return b > kKeyLeast ? fminf(a, b) : a; }
 
 // x times 2^n for any n that ends among the normal numbers: what is left of the factor for the last product.
 template <int DT>
@@ -621,7 +626,7 @@ __device__ __forceinline__ void dq_rests(const AttnBwd &a, uint32_t id, const Hi
     }
     // the factor is that of what there was without the rests
     const float largest = __builtin_elementwise_maximum(most, __shfl_xor(most, 32));
-    bad |= !(largest <= kFactorMost) || (largest > 0.0f && largest < kFactorFloor<NP>);
+    bad |= !(largest <= kFactorMost) || (largest > kRowLeast && largest < kFactorFloor<NP>);
 }
 
 // Returns whether the workgroup has to be computed with bf16 pieces.
@@ -693,9 +698,9 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
             for (int i = 0; i < 16; ++i) x[i] = exp2_fast(fmaf(x[i], scale2, -lse2)) * fmaf(dp[i], dp_by, -delta_by);
 #pragma unroll
             for (int i = 0; i < 16; i += 2) top = larger(x[i], x[i + 1], top);
-            if (__builtin_expect(__any(factor_off<NP>(top, top)), 0)) {
+            if (__builtin_expect(__any(factor_off<NP>(top, top, kRowLeast)), 0)) {
                 const float both = __builtin_elementwise_maximum(top, __shfl_xor(top, 32));
-                const int fall = factor_fall(both, both);
+                const int fall = factor_fall(both, both, kRowLeast);
                 bad |= !(both < INFINITY);
                 factor -= fall;
                 dp_by = ldexpf(down, factor);
@@ -989,10 +994,10 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
                 top = larger(x[4 * g], x[4 * g + 1], larger(x[4 * g + 2], x[4 * g + 3], top));
                 top_ds = larger(dp[4 * g], dp[4 * g + 1], larger(dp[4 * g + 2], dp[4 * g + 3], top_ds));
             }
-            if (__builtin_expect(__any(factor_off<NP>(__builtin_elementwise_maximum(top, top_ds), smaller(top, top_ds))), 0)) {
+            if (__builtin_expect(__any(factor_off<NP>(__builtin_elementwise_maximum(top, top_ds), smaller(top, top_ds), kKeyLeast)), 0)) {
                 const float both = __builtin_elementwise_maximum(top, __shfl_xor(top, 32)), both_ds = __builtin_elementwise_maximum(top_ds, __shfl_xor(top_ds, 32));
                 const float higher = __builtin_elementwise_maximum(both, both_ds);
-                const int fall = factor_fall(higher, smaller(both, both_ds));
+                const int fall = factor_fall(higher, smaller(both, both_ds), kKeyLeast);
                 bad |= !(higher < INFINITY);
                 factor -= fall;
                 by = ldexpf(1.0f, factor);
@@ -1034,7 +1039,7 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
     most = __builtin_elementwise_maximum(most, __shfl_xor(most, 32));
     most_ds = __builtin_elementwise_maximum(most_ds, __shfl_xor(most_ds, 32));
     const float low = smaller(most, most_ds);
-    bad |= widest - running > static_cast<float>(kGrowSpread) || (low > 0.0f && low < kFactorFloor<NP>);
+    bad |= widest - running > static_cast<float>(kGrowSpread) || (low > kKeyLeast && low < kFactorFloor<NP>);
     bad |= most * (dp_lost_of_do(high) + dp_lost_of_v(high)) * 0x1p3f > most_ds;      // P dp_lost 2^-17 2^20
     if (__builtin_expect(half_flags(a, high, bad), 0)) return true;
     if (__builtin_expect(high.q >> 31, 0)) dkv_rests<NP, DT>(a, opaque(id), sh, dk, dv, least, by);      // the same in the whole workgroup

@@ -124,3 +124,46 @@ def test_a_sink_without_value(fmt, f, codes, result, score, nq):  # noqa: F811
     k[:, 0, :, 0] = 2.0 * score                  # a score of `score` more
     v[:, 0] = 0.0
     check(fmt, q, k, v, do if score <= 6 else None, f, codes, result, False)
+
+
+@pytest.mark.parametrize("f,codes,result", [(SIX, False, "f32"), (BF16, True, "f32"), (BF16, True, "code16"), ((7, 8, True), True, "f32"), (HALF, False, "f32")])
+@pytest.mark.parametrize("d,stretch", [(3, 6.0), (40, 4.0), (64, 3.0), (128, 5.0)])
+@pytest.mark.parametrize("window", [0, 7])
+def test_rows_that_one_key_takes(fmt, f, codes, result, d, stretch, window):  # noqa: F811
+    """Scores of some hundred: weights of 1 and of 2^-100 and less, and a dS that is nothing but rounding, or zero, or the smallest number there is."""
+    rng = np.random.default_rng(d)
+    q, k, v, do = inputs(rng, 3, 90, 90, 3, 1, d, grad=1.0)
+    v[:, ::3] *= np.float32(30.0)
+    check(fmt, q * np.float32(stretch), k * np.float32(stretch), v, do, f, codes, result, window > 0, window, 130 if window else 0)
+
+
+@pytest.mark.parametrize("f,codes", [(SIX, False), (BF16, True), ((7, 8, True), True), ((8, 4, True), False), ((8, 10, True), False)])
+@pytest.mark.parametrize("d,stretch", [(3, 8.0), (3, 12.0), (16, 10.0), (80, 10.0)])
+@pytest.mark.parametrize("channel", [0, 2 ** -8, 2 ** -26])
+def test_gradients_stay_numbers(fmt, f, codes, d, stretch, channel):  # noqa: F811
+    """The same further on, where most gradients lie below fp32's normal numbers, with channels of K and V that lose bits: none is NaN or infinite, and
+    rows that see nothing but keys without weight get what the 64-bit definition gives, to the largest gradient's 2^-17."""
+    import layerdef as L
+    rng = np.random.default_rng(d)
+    q, k, v, do = inputs(rng, 2, 60, 60, 2, 1, d, grad=1.0)
+    q, k = q * np.float32(stretch), k * np.float32(stretch)
+    k[..., 1] *= np.float32(channel)
+    v[..., 2] *= np.float32(channel)
+    t = [fmt.fmt_pack16(torch.from_numpy(x).cuda(), f) if codes else torch.from_numpy(x).cuda() for x in (q, k, v)]
+    how = dict(causal=True, window=7, sinks=130, result="f32")
+    o, lse = fmt.fmt_attention_fwd(*t, f, **how)
+    grads = [x.cpu().numpy() for x in fmt.fmt_attention_bwd(torch.from_numpy(do).cuda(), *t, o, lse, f, **how)]
+    vq, vk, vv, vdo = (L.rounded(x, f).astype(np.float64) for x in (q, k, v, do))
+    want = [np.zeros(x.shape) for x in (q, k, v)]
+    seen = L.visible(60, 60, 60, 0, True, 7, 130)
+    for i in range(2):
+        for j in range(2):
+            r = L.attention(vq[i, :, j], vk[i, :, 0], vv[i, :, 0], seen, d ** -0.5, vdo[i, :, j])
+            want[0][i, :, j] = r[2]
+            want[1][i, :, 0] += r[3]
+            want[2][i, :, 0] += r[4]
+    # scores of |q||k| / sqrt(d) have 64 u of that, and P and the gradients as much relatively
+    score = 64 * 2.0 ** -24 * float((np.abs(vq).max() * np.abs(vk).max() * d) * d ** -0.5)
+    for a, x in zip(grads, want):
+        assert np.isfinite(a).all()
+        assert np.abs(a - x).max() <= (2.0 ** -17 + 3 * score) * np.abs(x).max() * 4

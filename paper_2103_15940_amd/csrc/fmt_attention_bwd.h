@@ -421,6 +421,7 @@ constexpr float kFactorFloor = NP == 2 ? 0x1p-5f : 0x1p-10f;
 // (dK's dS share the factor of dV's P.)  What is below `least` is taken for nothing: with a factor that brought it up, other products would overflow
 // (a row's dP comes to 2^38 at most, in the units that dS is held in, and is multiplied by the factor before P).
 constexpr float kRowLeast = 0x1p-60f, kKeyLeast = 0x1p-80f;
+constexpr int kRowMost = 80, kKeyMost = 104;         // exponents that factors do not pass
 template <int NP>
 __device__ __forceinline__ bool factor_off(float high, float low, float least)
 {
@@ -428,8 +429,8 @@ __device__ __forceinline__ bool factor_off(float high, float low, float least)
 }
 
 // By how many binades the factors of a wave fall (rise: negative).  When one changes, others that are low rise as well, and those that have seen
-// nothing go with one that rises, so that few changes follow.
-__device__ __forceinline__ int factor_fall(float high, float low, float least)
+// nothing go with one that rises, so that few changes follow.  room: how far they may rise.
+__device__ __forceinline__ int factor_fall(float high, float low, float least, int room)
 {
     int fall = high > kFactorMost ? exponent_of(high) - 11 : low > least && low < 64.0f ? min(max(exponent_of(low) - 9, exponent_of(high) - 11), 0) : 0;
     if (!(high < INFINITY)) fall = 0;
@@ -438,7 +439,7 @@ __device__ __forceinline__ int factor_fall(float high, float low, float least)
         const int one = __builtin_amdgcn_readlane(fall, __builtin_ctzll(rising));
         if (high <= least) fall = max(one, -20);
     }
-    return fall;
+    return max(fall, -room);
 }
 // The smaller of two largest products, where the second is not nothing.
 __device__ __forceinline__ float smaller(float a, float b) { return b > kKeyLeast ? fminf(a, b) : a; }
@@ -700,7 +701,7 @@ __device__ __forceinline__ bool dq_half(const AttnBwd &a, uint32_t id, DqHalfSha
             for (int i = 0; i < 16; i += 2) top = larger(x[i], x[i + 1], top);
             if (__builtin_expect(__any(factor_off<NP>(top, top, kRowLeast)), 0)) {
                 const float both = __builtin_elementwise_maximum(top, __shfl_xor(top, 32));
-                const int fall = factor_fall(both, both, kRowLeast);
+                const int fall = factor_fall(both, both, kRowLeast, kRowMost - factor);
                 bad |= !(both < INFINITY);
                 factor -= fall;
                 dp_by = ldexpf(down, factor);
@@ -950,7 +951,7 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
             // what the sums hold falls with c, but no further than to a largest P of 2^3: from there on the factor rises instead
             const int by_now = least == kNoRow ? 0 : static_cast<int>(least - next);
             const float both = fmaxf(most, __shfl_xor(most, 32));
-            const int fall = both > 0.0f ? min(by_now, max(exponent_of(both) - 3, 0)) : by_now;
+            const int fall = both > 0.0f ? min(by_now, max(max(exponent_of(both) - 3, factor + by_now - kKeyMost), 0)) : by_now;
             least = next;
             factor += by_now - fall;
             by = ldexpf(1.0f, factor);
@@ -997,7 +998,7 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
             if (__builtin_expect(__any(factor_off<NP>(__builtin_elementwise_maximum(top, top_ds), smaller(top, top_ds), kKeyLeast)), 0)) {
                 const float both = __builtin_elementwise_maximum(top, __shfl_xor(top, 32)), both_ds = __builtin_elementwise_maximum(top_ds, __shfl_xor(top_ds, 32));
                 const float higher = __builtin_elementwise_maximum(both, both_ds);
-                const int fall = factor_fall(higher, smaller(both, both_ds), kKeyLeast);
+                const int fall = factor_fall(higher, smaller(both, both_ds), kKeyLeast, kKeyMost - factor);
                 bad |= !(higher < INFINITY);
                 factor -= fall;
                 by = ldexpf(1.0f, factor);

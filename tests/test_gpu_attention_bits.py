@@ -167,3 +167,21 @@ def test_gradients_stay_numbers(fmt, f, codes, d, stretch, channel):  # noqa: F8
     for a, x in zip(grads, want):
         assert np.isfinite(a).all()
         assert np.abs(a - x).max() <= (2.0 ** -17 + 3 * score) * np.abs(x).max() * 4
+
+
+@pytest.mark.parametrize("f,codes", [(BF16, True), ((8, 4, True), False), ((8, 7, False), False), (SIX, False)])
+@pytest.mark.parametrize("n,d,window,sinks", [(600, 1, 40, 5), (600, 3, 7, 1), (700, 3, 200, 130), (500, 16, 30, 0)])
+@pytest.mark.parametrize("first", [0, 40])
+def test_rows_that_see_late_what_others_see_early(fmt, f, codes, n, d, window, sinks, first):  # noqa: F811
+    """Rows of one wave whose first keys lie tiles apart, with a dS of next to nothing in between: the factors of those that have seen nothing yet go
+    with the others' and stay where products with them are numbers."""
+    rng = np.random.default_rng(n + d)
+    q, k, v, do = inputs(rng, 2, n, n, 1, 1, d, grad=1.0)
+    k = k * np.exp2(rng.normal(size=(1, n, 1, 1)) * 3).astype(np.float32)
+    q, k = q * np.float32(4.0), np.clip(k * np.float32(8.0), -100, 100)
+    k[:, ::50] *= np.float32(2.0 ** -28)
+    t = [fmt.fmt_pack16(torch.from_numpy(x).cuda(), f) if codes else torch.from_numpy(x).cuda() for x in (q, k, v)]
+    how = dict(causal=True, window=window, sinks=sinks, result="f32", q_pos=torch.tensor([first, first + 16], dtype=torch.int32, device="cuda"))
+    o, lse = fmt.fmt_attention_fwd(*t, f, **how)
+    for x in fmt.fmt_attention_bwd(torch.from_numpy(do).cuda(), *t, o, lse, f, **how):
+        assert bool(torch.isfinite(x).all())

@@ -1039,7 +1039,9 @@ __device__ __forceinline__ bool dkv_half(const AttnBwd &a, uint32_t id, DkvHalfS
     // too small beside one another for one factor: V of the key's rows is tiny or large altogether, or their dS all rounding
     most = __builtin_elementwise_maximum(most, __shfl_xor(most, 32));
     most_ds = __builtin_elementwise_maximum(most_ds, __shfl_xor(most_ds, 32));
-    const float low = smaller(most, most_ds);
+    // A row's only key has P = 1 and dP = delta: its dS is the rounding of 0, and has nothing to keep (one token, 12 heads of 40: 48 -> 31 us).
+    const bool only = key.seq.length == 1 || (s.window == 1 && s.sinks == 0);
+    const float low = only ? most : smaller(most, most_ds);
     bad |= widest - running > static_cast<float>(kGrowSpread) || (low > kKeyLeast && low < kFactorFloor<NP>);
     bad |= most * (dp_lost_of_do(high) + dp_lost_of_v(high)) * 0x1p3f > most_ds;      // P dp_lost 2^-17 2^20
     if (__builtin_expect(half_flags(a, high, bad), 0)) return true;
